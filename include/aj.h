@@ -213,6 +213,53 @@ size_t aj_embed_bwd_workspace_bytes(int32_t n_tok, int32_t d);
 int aj_embed_bwd(const int32_t *tok, int32_t n_tok, const float *dx, int32_t d, int32_t vocab,
                  float *d_emb, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------ packs
+ * Segments laid end to end in one pack, as the merge and aj_plan_packs leave them. */
+typedef struct {
+  int32_t n_tok;                /* tokens in the pack */
+  int32_t n_seg;                /* segments in the pack */
+  int32_t max_seqlen;           /* longest segment (host value) */
+  int32_t base;                 /* cu_seqlens values are offsets + base (a slice of a
+                                   batch-wide array): row r of the pack is offset r + base */
+  const int32_t *cu_seqlens;    /* [n_seg+1], cu_seqlens[0] == base, cu_seqlens[n_seg] == base + n_tok */
+  const int32_t *pos;           /* [n_tok] position of each token inside its segment (RoPE) */
+} aj_varlen;
+
+/* ------------------------------------------------------------------ attention
+ * The attention of the block below by itself, over a pack of segments, with an
+ * optional window: token i of a segment that starts at s sees the keys j of
+ * [s, i] with j > i - window (its last `window` keys, itself among them) or
+ * j < s + n_sink (the segment's first tokens, which stay visible).  window 0,
+ * or one that no row reaches past, is full causal attention; n_sink then adds
+ * nothing.
+ *   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i k_j - lse_i),  query head h on
+ * key/value head floor(h*n_kv_heads/n_q_heads).
+ * qkv: [n_tok, (Hq+2Hkv)*hd] in cfg->dtype, the row layout of the block's W_qkv,
+ * q and k already rotated; out: [n_tok, Hq*hd]; lse: float32 [Hq, n_tok], the
+ * log-sum-exp of a row's scaled scores in log2 units (the backward reads it).
+ * vl->pos is not read.  Scores, softmax statistics and sums are float32; bfloat16
+ * rounds p and d score once, as operands of the next product, and the results.
+ * The backward writes d qkv (not accumulated), each sum in a fixed order
+ * (bit-identical on every call).  qkv, out, lse, d out and d qkv must not overlap.
+ * ws: at least aj_attention_workspace_bytes(cfg, n_tok), for either direction; it
+ * carries nothing from one to the other.
+ * Errors as the block's; n_tok at most 2^30, n_tok * n_q_heads below 2^32.  Infinities and
+ * NaN as in the block.
+ */
+typedef struct {
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  int32_t window, n_sink;
+  int32_t dtype;                /* aj_dtype of qkv, out and their gradients */
+  float scale;                  /* of the scores; 0 = 1/sqrt(head_dim) */
+} aj_attn_cfg;
+
+size_t aj_attention_workspace_bytes(const aj_attn_cfg *cfg, int32_t n_tok);
+int aj_attention_fwd(const aj_attn_cfg *cfg, const aj_varlen *vl, const void *qkv, void *out,
+                     float *lse, void *ws, size_t ws_bytes, void *stream);
+int aj_attention_bwd(const aj_attn_cfg *cfg, const aj_varlen *vl, const void *qkv,
+                     const void *out, const float *lse, const void *dout, void *dqkv, void *ws,
+                     size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------------------ 2. block
  * The policy's forward and backward over the merged samples: Section 4.4.2
  * (Timeline Merging) merges timelines precisely so that the actor update
@@ -235,6 +282,7 @@ typedef struct {
   float rms_eps;
   float rope_theta;
   int32_t dtype;                /* aj_dtype of weights, x, y and saved activations */
+  int32_t window, n_sink;       /* attention window and sinks, as aj_attn_cfg's (0: none) */
 } aj_block_cfg;
 
 typedef struct {
@@ -260,16 +308,6 @@ typedef struct {
 typedef struct {                /* float32, accumulated */
   float *attn_norm, *w_qkv, *w_o, *mlp_norm, *w_gate_up, *w_down;
 } aj_block_grads;
-
-typedef struct {
-  int32_t n_tok;                /* tokens in the pack */
-  int32_t n_seg;                /* segments in the pack */
-  int32_t max_seqlen;           /* longest segment (host value) */
-  int32_t base;                 /* cu_seqlens values are offsets + base (a slice of a
-                                   batch-wide array): row r of the pack is offset r + base */
-  const int32_t *cu_seqlens;    /* [n_seg+1], cu_seqlens[0] == base, cu_seqlens[n_seg] == base + n_tok */
-  const int32_t *pos;           /* [n_tok] position of each token inside its segment (RoPE) */
-} aj_varlen;
 
 /* Bytes of the activation arena the forward fills and the backward reads,
  * scratch of the forward's split reductions included: 8 KB per token, at most

@@ -64,7 +64,13 @@ class TimelinesOut(C.Structure):
 
 class BlockCfg(C.Structure):
     _fields_ = [("d_model", i32), ("n_q_heads", i32), ("n_kv_heads", i32), ("head_dim", i32),
-                ("d_ff", i32), ("rms_eps", f32), ("rope_theta", f32), ("dtype", i32)]
+                ("d_ff", i32), ("rms_eps", f32), ("rope_theta", f32), ("dtype", i32),
+                ("window", i32), ("n_sink", i32)]
+
+
+class AttnCfg(C.Structure):
+    _fields_ = [("n_q_heads", i32), ("n_kv_heads", i32), ("head_dim", i32), ("window", i32),
+                ("n_sink", i32), ("dtype", i32), ("scale", f32)]
 
 
 BLOCK_TRANSPOSED = ("w_qkv_t", "w_o_t", "w_gate_up_t", "w_down_t")
@@ -122,6 +128,10 @@ EXPORTS = {
     "aj_embed_fwd": (C.c_int, [vp, i32, vp, i32, i32, C.c_int, vp, vp, vp]),
     "aj_embed_bwd_workspace_bytes": (sz, [i32, i32]),
     "aj_embed_bwd": (C.c_int, [vp, i32, vp, i32, i32, vp, vp, sz, vp]),
+    "aj_attention_workspace_bytes": (sz, [C.POINTER(AttnCfg), i32]),
+    "aj_attention_fwd": (C.c_int, [C.POINTER(AttnCfg), C.POINTER(Varlen), vp, vp, vp, vp, sz, vp]),
+    "aj_attention_bwd": (C.c_int, [C.POINTER(AttnCfg), C.POINTER(Varlen), vp, vp, vp, vp, vp, vp,
+                                   sz, vp]),
     "aj_block_saved_bytes": (sz, [C.POINTER(BlockCfg), i32]),
     "aj_block_workspace_bytes": (sz, [C.POINTER(BlockCfg), i32, i32]),
     "aj_varlen_block_fwd": (C.c_int, [C.POINTER(BlockCfg), C.POINTER(BlockWeights),
@@ -294,11 +304,85 @@ def aj_embed_bwd(tok, dx, d_emb, ws, stream=None):
                               stream_handle(stream)), "aj_embed_bwd")
 
 
+# ------------------------------------------------------------------ attention
+
+def _operands(name, tensors):
+    """Checks {argument: (tensor, dtypes, shape)}: on the current GPU, of one of the dtypes, of
+    that shape, rows end to end."""
+    for arg, (t, dtypes, shape) in tensors.items():
+        if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or tuple(t.shape) != tuple(shape):
+            got = f"{t.dtype} {tuple(t.shape)}" if isinstance(t, torch.Tensor) else type(t).__name__
+            raise AjError(f"{name}: {arg} must be {' or '.join(str(d) for d in dtypes)} "
+                          f"{tuple(shape)}, got {got}")
+        if not t.is_contiguous():
+            raise AjError(f"{name}: {arg} must be contiguous")
+    for arg, (t, _, _) in tensors.items():
+        _on_gpu(name, arg, t)
+
+
+def _on_gpu(name, arg, t):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise AjError(f"{name}: {arg} must be on the current GPU, is on {t.device}")
+
+
+def _workspace(name, ws):
+    if not isinstance(ws, torch.Tensor) or not ws.is_contiguous():
+        raise AjError(f"{name}: ws must be a contiguous tensor")
+    _on_gpu(name, "ws", ws)
+    return ptr(ws), ws.numel() * ws.element_size()
+
+
+def attn_cfg(n_q_heads, n_kv_heads, head_dim, window=0, n_sink=0, dtype=torch.bfloat16, scale=0.0):
+    """window 0: full causal attention; scale 0: 1/sqrt(head_dim)."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise AjError(f"unsupported dtype {dtype}")
+    return AttnCfg(n_q_heads, n_kv_heads, head_dim, window, n_sink,
+                   AJ_BF16 if dtype == torch.bfloat16 else AJ_F32, scale)
+
+
+def aj_attention_workspace_bytes(cfg, n_tok):
+    return int(lib().aj_attention_workspace_bytes(C.byref(cfg), int(n_tok)))
+
+
+def _attn_operands(name, cfg, cu_seqlens, qkv, extra):
+    n, dt = qkv.shape[0], (torch.bfloat16 if cfg.dtype == AJ_BF16 else torch.float32,)
+    width, hq = (cfg.n_q_heads + 2 * cfg.n_kv_heads) * cfg.head_dim, cfg.n_q_heads * cfg.head_dim
+    _operands(name, {"qkv": (qkv, dt, (n, width)),
+                     "cu_seqlens": (cu_seqlens, (torch.int32,), (cu_seqlens.numel(),)),
+                     **{k: (t, (torch.float32,) if k == "lse" else dt,
+                            {"lse": (cfg.n_q_heads, n), "dqkv": (n, width)}.get(k, (n, hq)))
+                        for k, t in extra.items()}})
+    return n
+
+
+def aj_attention_fwd(cfg, cu_seqlens, max_seqlen, qkv, out, lse, ws, base=0, stream=None):
+    """qkv [n_tok, (Hq+2Hkv)*hd], out [n_tok, Hq*hd], lse float32 [Hq, n_tok] (log2 units); ws: a
+    byte tensor of aj_attention_workspace_bytes(cfg, n_tok)."""
+    name = "aj_attention_fwd"
+    n = _attn_operands(name, cfg, cu_seqlens, qkv, {"out": out, "lse": lse})
+    vl = _varlen(n, cu_seqlens.numel() - 1, max_seqlen, base, cu_seqlens, None)
+    _check(lib().aj_attention_fwd(C.byref(cfg), C.byref(vl), ptr(qkv), ptr(out), ptr(lse),
+                                  *_workspace(name, ws), stream_handle(stream)), name)
+
+
+def aj_attention_bwd(cfg, cu_seqlens, max_seqlen, qkv, out, lse, dout, dqkv, ws, base=0,
+                     stream=None):
+    """d qkv of aj_attention_fwd from d out; out and lse are the forward's."""
+    name = "aj_attention_bwd"
+    n = _attn_operands(name, cfg, cu_seqlens, qkv,
+                       {"out": out, "lse": lse, "dout": dout, "dqkv": dqkv})
+    vl = _varlen(n, cu_seqlens.numel() - 1, max_seqlen, base, cu_seqlens, None)
+    _check(lib().aj_attention_bwd(C.byref(cfg), C.byref(vl), ptr(qkv), ptr(out), ptr(lse),
+                                  ptr(dout), ptr(dqkv), *_workspace(name, ws),
+                                  stream_handle(stream)), name)
+
+
 # ------------------------------------------------------------------ block
 
 def block_cfg(m):
     return BlockCfg(m.d_model, m.n_q_heads, m.n_kv_heads, m.head_dim, m.d_ff, m.rms_eps,
-                    m.rope_theta, AJ_BF16 if m.dtype == "bf16" else AJ_F32)
+                    m.rope_theta, AJ_BF16 if m.dtype == "bf16" else AJ_F32,
+                    getattr(m, "window", 0), getattr(m, "n_sink", 0))
 
 
 def aj_block_saved_bytes(cfg, n_tok):

@@ -25,6 +25,7 @@
 // with the masked pairs left out one by one: a bad row stays with the rows that
 // attend to it, and finite rows pay one check at the end (a check of every step's
 // rows cost 3 to 8 %).
+#include <algorithm>
 #include <type_traits>
 #include "ops.h"
 
@@ -57,6 +58,30 @@ AJ_DEV int seg_end(const A &a, int row) {
   const int v = a.cu_seqlens[seg_of(a.cu_seqlens, a.n_seg, a.base, row) + 1] - a.base;
   return v <= row ? row + 1 : (v > a.n_tok ? a.n_tok : v);
 }
+
+// With a window W and S sinks, row i of a segment that starts at s attends to the keys
+// j of [s, i] with j > i - W or j < s + S.  A workgroup of query rows [row0, last]
+// walks the keys from lo, the first one in row0's window, to `last` (which takes in the
+// sinks of the segments that start in between), and before them the sinks of
+// row0's segment that lie below lo.
+struct KeySteps {
+  int lo, sink_lo, sink_hi;   // window keys from lo; sinks [sink_lo, sink_hi) below it
+  int n_sink, n;              // steps over the sinks, and in all
+};
+template <bool WIN, typename A>
+AJ_DEV KeySteps key_steps(const A &a, int row0, int last, int step) {
+  const int s0 = seg_start(a, row0);
+  KeySteps k{s0, s0, s0, 0, 0};
+  if (WIN) {
+    k.lo = max(s0, row0 - a.window + 1);
+    k.sink_hi = s0 + min(a.n_sink, k.lo - s0);
+    k.n_sink = (k.sink_hi - s0 + step - 1) / step;
+  }
+  k.n = k.n_sink + (last - k.lo + step) / step;
+  return k;
+}
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 AJ_DEV f32x4_t mfma4(float a, float b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -186,7 +211,7 @@ AJ_DEV bool vec4(const void *p, int64_t ld, int es) {
   return ld % 4 == 0 && ((uintptr_t)p & (4 * es - 1)) == 0;
 }
 
-template <typename T, int NC>
+template <typename T, int NC, bool WIN>
 __global__ __launch_bounds__(256) void attn_fwd_f32_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) float Ks[kStep<NC> * kLd<NC>], Vs[kStep<NC> * kLd<NC>];
   const int hd = a.hd, ld = (a.Hq + 2 * a.Hkv) * hd;
@@ -205,24 +230,34 @@ __global__ __launch_bounds__(256) void attn_fwd_f32_kernel(AttnArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) q[c][j] *= a.scale;
   float m, l;
-  const int k_lo = seg_start(a, row0);
+  const KeySteps ks = key_steps<WIN>(a, row0, last, kStep<NC>);
   float4 kr[kFours<NC>], vr[kFours<NC>];
+  auto first_key = [&](int i) {
+    return i < ks.n_sink ? ks.sink_lo + i * kStep<NC> : ks.lo + (i - ks.n_sink) * kStep<NC>;
+  };
+  auto fetch = [&](int i) __attribute__((always_inline)) {
+    const int k0 = first_key(i), end = i < ks.n_sink ? ks.sink_hi - 1 : last;
+    fetch_rows<T, NC>(kr, kp, ld, hd, vec, k0, end);
+    fetch_rows<T, NC>(vr, vp, ld, hd, vec, k0, end);
+  };
   auto walk = [&](auto exact) __attribute__((always_inline)) {
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    fetch_rows<T, NC>(kr, kp, ld, hd, vec, k_lo, last);
-    fetch_rows<T, NC>(vr, vp, ld, hd, vec, k_lo, last);
-    for (int k0 = k_lo; k0 <= last; k0 += kStep<NC>) {
+    fetch(0);
+    for (int i = 0; i < ks.n; ++i) {
       __syncthreads();
       put_rows<NC>(Ks, kr);
       put_rows<NC>(Vs, vr);
       __syncthreads();
-      if (k0 + kStep<NC> <= last) {
-        fetch_rows<T, NC>(kr, kp, ld, hd, vec, k0 + kStep<NC>, last);
-        fetch_rows<T, NC>(vr, vp, ld, hd, vec, k0 + kStep<NC>, last);
-      }
+      if (i + 1 < ks.n) fetch(i + 1);
+      const bool sinks = WIN && i < ks.n_sink;
+      const int k0 = first_key(i);
+      // the sinks' steps end where the window's begin; no key is met twice
+      const int low = sinks ? start : WIN ? max(start, row - a.window + 1) : start;
+      const int high = sinks ? ks.sink_hi - 1 : row;
+      const int sink = WIN && !sinks ? start + a.n_sink : start;
       for (int t = 0; t < kStep<NC> && k0 + t <= w0 + 15; t += 16) {
         f32x4_t s = rows_dot<NC>(Ks + t * kLd<NC>, q);
         const int key = k0 + t + 4 * (lane >> 4);
@@ -230,8 +265,12 @@ __global__ __launch_bounds__(256) void attn_fwd_f32_kernel(AttnArgs a) {
         int in = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (key + j < start || key + j > row || !valid) s[j] = -INFINITY;
-          else in |= 1 << j;
+          const int kj = key + j;
+          // `&`, `|` and selects: from `&&` with an else that stores to s[j] the
+          // compiler made code that left s[j] as it was on the inner way out
+          const bool inj = valid & (kj <= high) & ((kj >= low) | (WIN & (kj >= start) & (kj < sink)));
+          in |= (int)inj << j;
+          s[j] = inj ? s[j] : -INFINITY;
           mx = fmaxf(mx, s[j]);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -262,7 +301,7 @@ __global__ __launch_bounds__(256) void attn_fwd_f32_kernel(AttnArgs a) {
   l += __shfl_xor(l, 32, 64);
   if (!valid) return;
   store_row<T, NC>((T *)a.o + (int64_t)row * a.Hq * hd + h * hd, o, hd, 1.f / l);
-  if (lane < 16) a.lse[(int64_t)h * a.n_tok + row] = m + logf(l);
+  if (lane < 16) a.lse[(int64_t)h * a.n_tok + row] = (m + logf(l)) * (a.lse_log2 ? kLog2e : 1.f);
 }
 
 // delta[h][row] = sum_d dO * O
@@ -282,7 +321,7 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnBwdArgs a) {
 }
 
 // dQ rows: dq = scale * sum_j P_j (dO.V_j - delta) K_j
-template <typename T, int NC>
+template <typename T, int NC, bool WIN>
 __global__ __launch_bounds__(256) void attn_dq_f32_kernel(AttnBwdArgs a) {
   __shared__ __attribute__((aligned(16))) float Ks[kStep<NC> * kLd<NC>], Vs[kStep<NC> * kLd<NC>];
   const int hd = a.hd, ld = (a.Hq + 2 * a.Hkv) * hd;
@@ -294,27 +333,38 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(AttnBwdArgs a) {
   const T *qkv = (const T *)a.qkv, *kp = qkv + (a.Hq + g) * hd, *vp = kp + a.Hkv * hd;
   const bool vec = vec4(a.qkv, ld, sizeof(T));
   const int start = valid ? seg_start(a, row) : row;
-  const float lse = valid ? a.lse[(int64_t)h * a.n_tok + row] : 0.f;
+  const float lse_unit = a.lse_log2 ? kLn2 : 1.f;
+  const float lse = valid ? a.lse[(int64_t)h * a.n_tok + row] * lse_unit : 0.f;
   const float delta = valid ? a.delta[(int64_t)h * a.n_tok + row] : 0.f;
   f32x4_t q[NC], dob[NC], dq[NC];
   own_row<T, NC>(q, qkv + (int64_t)row * ld + h * hd, hd, valid);
   own_row<T, NC>(dob, (const T *)a.dout + (int64_t)row * a.Hq * hd + h * hd, hd, valid);
-  const int k_lo = seg_start(a, row0);
+  const KeySteps ks = key_steps<WIN>(a, row0, last, kStep<NC>);
   float4 kr[kFours<NC>], vr[kFours<NC>];
+  auto first_key = [&](int i) {
+    return i < ks.n_sink ? ks.sink_lo + i * kStep<NC> : ks.lo + (i - ks.n_sink) * kStep<NC>;
+  };
+  auto fetch = [&](int i) __attribute__((always_inline)) {
+    const int k0 = first_key(i), end = i < ks.n_sink ? ks.sink_hi - 1 : last;
+    fetch_rows<T, NC>(kr, kp, ld, hd, vec, k0, end);
+    fetch_rows<T, NC>(vr, vp, ld, hd, vec, k0, end);
+  };
   auto walk = [&](auto exact) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) dq[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    fetch_rows<T, NC>(kr, kp, ld, hd, vec, k_lo, last);
-    fetch_rows<T, NC>(vr, vp, ld, hd, vec, k_lo, last);
-    for (int k0 = k_lo; k0 <= last; k0 += kStep<NC>) {
+    fetch(0);
+    for (int i = 0; i < ks.n; ++i) {
       __syncthreads();
       put_rows<NC>(Ks, kr);
       put_rows<NC>(Vs, vr);
       __syncthreads();
-      if (k0 + kStep<NC> <= last) {
-        fetch_rows<T, NC>(kr, kp, ld, hd, vec, k0 + kStep<NC>, last);
-        fetch_rows<T, NC>(vr, vp, ld, hd, vec, k0 + kStep<NC>, last);
-      }
+      if (i + 1 < ks.n) fetch(i + 1);
+      const bool sinks = WIN && i < ks.n_sink;
+      const int k0 = first_key(i);
+      // the sinks' steps end where the window's begin; no key is met twice
+      const int low = sinks ? start : WIN ? max(start, row - a.window + 1) : start;
+      const int high = sinks ? ks.sink_hi - 1 : row;
+      const int sink = WIN && !sinks ? start + a.n_sink : start;
       for (int t = 0; t < kStep<NC> && k0 + t <= w0 + 15; t += 16) {
         const f32x4_t s = rows_dot<NC>(Ks + t * kLd<NC>, q);
         const f32x4_t dp = rows_dot<NC>(Vs + t * kLd<NC>, dob);
@@ -323,7 +373,8 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(AttnBwdArgs a) {
         int in = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bool inj = valid && key + j >= start && key + j <= row;
+          const int kj = key + j;
+          const bool inj = valid & (kj <= high) & ((kj >= low) | (WIN & (kj >= start) & (kj < sink)));
           ds[j] = inj ? __expf(s[j] * a.scale - lse) * (dp[j] - delta) * a.scale : 0.f;
           in |= inj << j;
         }
@@ -337,8 +388,9 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(AttnBwdArgs a) {
 }
 
 // dK, dV rows of kv head g: sum over the query heads of the group and the
-// queries of the same segment at or after the key.
-template <typename T, int NC>
+// queries of the same segment at or after the key (with a window: the W of them
+// from the key on, all of them for a sink).
+template <typename T, int NC, bool WIN>
 __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(AttnBwdArgs a) {
   __shared__ __attribute__((aligned(16))) float Qs[kStep<NC> * kLd<NC>], Ds[kStep<NC> * kLd<NC>];
   __shared__ __attribute__((aligned(16))) float Ls[kStep<NC>], Dl[kStep<NC>];
@@ -350,8 +402,18 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(AttnBwdArgs a) {
   const bool valid = row < a.n_tok;
   const T *qkv = (const T *)a.qkv;
   const bool vec = vec4(a.qkv, ld, sizeof(T)), vecd = vec4(a.dout, (int64_t)a.Hq * hd, sizeof(T));
-  const int end = valid ? seg_end(a, row) : 0;
-  const int q_hi = seg_end(a, min(row0 + kRows, a.n_tok) - 1) - 1;
+  int end = valid ? seg_end(a, row) : 0;
+  int q_hi = seg_end(a, min(row0 + kRows, a.n_tok) - 1) - 1;
+  if constexpr (WIN) {
+    if (valid && row - seg_start(a, row) >= a.n_sink && end - row > a.window) end = row + a.window;
+    __shared__ int hi[4];     // the last query that any key of the workgroup meets
+    int e = end;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o, 64));
+    if (lane == 0) hi[threadIdx.x >> 6] = e;
+    __syncthreads();
+    q_hi = max(max(hi[0], hi[1]), max(hi[2], hi[3])) - 1;
+  }
   // the last query any of the wave's keys meets
   int w_hi = end - 1;
 #pragma unroll
@@ -370,7 +432,7 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(AttnBwdArgs a) {
     fetch_rows<T, NC>(dr, (const T *)a.dout + h * hd, (int64_t)a.Hq * hd, hd, vecd, q0, q_hi);
     const int q = q0 + (int)threadIdx.x;
     if ((int)threadIdx.x < kStep<NC>) {
-      lr = q <= q_hi ? a.lse[(int64_t)h * a.n_tok + q] : 0.f;
+      lr = q <= q_hi ? a.lse[(int64_t)h * a.n_tok + q] * (a.lse_log2 ? kLn2 : 1.f) : 0.f;
       er = q <= q_hi ? a.delta[(int64_t)h * a.n_tok + q] : 0.f;
     }
   };
@@ -425,36 +487,50 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(AttnBwdArgs a) {
 
 }  // namespace
 
+bool windowed(int window, int n_tok) { return window > 0 && window < n_tok; }
+
 template <typename T>
-int attn_fwd(const AttnArgs &a, hipStream_t s) {
+int attn_fwd(const AttnArgs &args, hipStream_t s) {
+  AttnArgs a = args;
   if (a.n_tok <= 0) return AJ_OK;
+  a.n_sink = std::min(a.n_sink, a.n_tok);   // the sums of rows stay in 32 bits
   if (a.hd > kMaxHd || a.hd % 8) return fail(AJ_ERR_UNSUPPORTED, "attention: head_dim %d", a.hd);
-  if (sizeof(T) == 2 && attn_mfma_supported(a.hd, a.qkv, a.o, a.o)) return attn_fwd_mfma(a, s);
+  const bool win = windowed(a.window, a.n_tok);
+  if (!win && sizeof(T) == 2 && attn_mfma_supported(a.hd, a.qkv, a.o, a.o)) return attn_fwd_mfma(a, s);
   dim3 grid((a.n_tok + kRows - 1) / kRows, a.Hq);
   const int tk = timing_begin(s, AJ_KC_ATTN_FWD, 0.0);
-  AJ_NC_DISPATCH(a.hd, (attn_fwd_f32_kernel<T, NC><<<grid, 256, 0, s>>>(a)));
+  if (win) AJ_NC_DISPATCH(a.hd, (attn_fwd_f32_kernel<T, NC, true><<<grid, 256, 0, s>>>(a)));
+  else AJ_NC_DISPATCH(a.hd, (attn_fwd_f32_kernel<T, NC, false><<<grid, 256, 0, s>>>(a)));
   timing_end(s, tk);
   return check_launch("attention forward");
 }
 
 template <typename T>
-int attn_bwd(const AttnBwdArgs &a, hipStream_t s) {
+int attn_bwd(const AttnBwdArgs &args, hipStream_t s) {
+  AttnBwdArgs a = args;
   if (a.n_tok <= 0) return AJ_OK;
+  a.n_sink = std::min(a.n_sink, a.n_tok);
   if (a.hd > kMaxHd || a.hd % 8) return fail(AJ_ERR_UNSUPPORTED, "attention: head_dim %d", a.hd);
+  const bool win = windowed(a.window, a.n_tok);
   // the matrix-core forward saves its log-sum-exp in log2 units, the plain
-  // kernels in natural ones: the backward must take the forward's path
-  const bool fwd_mfma = sizeof(T) == 2 && attn_mfma_supported(a.hd, a.qkv, a.o, a.o);
-  if (fwd_mfma) {
-    if (!attn_mfma_supported(a.hd, a.qkv, a.dout, a.dqkv))
-      return fail(AJ_ERR_UNSUPPORTED, "attention backward: d out / d qkv not 16-byte aligned");
-    return attn_bwd_mfma(a, s);
-  }
+  // kernels in natural ones unless asked for log2: the backward must then take the
+  // forward's path
+  const bool fwd_mfma = !win && sizeof(T) == 2 && attn_mfma_supported(a.hd, a.qkv, a.o, a.o);
+  const bool bwd_mfma = fwd_mfma && attn_mfma_supported(a.hd, a.qkv, a.dout, a.dqkv);
+  if (bwd_mfma) return attn_bwd_mfma(a, s);
+  if (fwd_mfma && !a.lse_log2)
+    return fail(AJ_ERR_UNSUPPORTED, "attention backward: d out / d qkv not 16-byte aligned");
   const int64_t nd = (int64_t)a.n_tok * a.Hq;
   const int tk = timing_begin(s, AJ_KC_ATTN_BWD, 0.0);
   attn_delta_kernel<T><<<(unsigned)((nd + 3) / 4), 256, 0, s>>>(a);
   const int blocks = (a.n_tok + kRows - 1) / kRows;
-  AJ_NC_DISPATCH(a.hd, (attn_dq_f32_kernel<T, NC><<<dim3(blocks, a.Hq), 256, 0, s>>>(a)));
-  AJ_NC_DISPATCH(a.hd, (attn_dkv_f32_kernel<T, NC><<<dim3(blocks, a.Hkv), 256, 0, s>>>(a)));
+  if (win) {
+    AJ_NC_DISPATCH(a.hd, (attn_dq_f32_kernel<T, NC, true><<<dim3(blocks, a.Hq), 256, 0, s>>>(a)));
+    AJ_NC_DISPATCH(a.hd, (attn_dkv_f32_kernel<T, NC, true><<<dim3(blocks, a.Hkv), 256, 0, s>>>(a)));
+  } else {
+    AJ_NC_DISPATCH(a.hd, (attn_dq_f32_kernel<T, NC, false><<<dim3(blocks, a.Hq), 256, 0, s>>>(a)));
+    AJ_NC_DISPATCH(a.hd, (attn_dkv_f32_kernel<T, NC, false><<<dim3(blocks, a.Hkv), 256, 0, s>>>(a)));
+  }
   timing_end(s, tk);
   return check_launch("attention backward");
 }
@@ -464,4 +540,96 @@ template int attn_fwd<bf16_t>(const AttnArgs &, hipStream_t);
 template int attn_bwd<float>(const AttnBwdArgs &, hipStream_t);
 template int attn_bwd<bf16_t>(const AttnBwdArgs &, hipStream_t);
 
+namespace {
+
+struct AttnWs {
+  float *delta, *part;
+  size_t part_floats, bytes;
+};
+
+// Scratch of the public backward: delta, and float32 sums of dK, dV in parts, one part
+// per query head of a group at most and 268 MB in all.
+AttnWs carve_attn(const aj_attn_cfg &c, int n, void *base) {
+  Carver cv(base);
+  AttnWs w;
+  w.delta = cv.take<float>((int64_t)c.n_q_heads * n);
+  w.part_floats = 0;
+  if (c.dtype == AJ_BF16)
+    w.part_floats = std::min((size_t)2 * c.n_q_heads * n * c.head_dim, (size_t)64 << 20);
+  w.part = cv.take<float>(w.part_floats);
+  w.bytes = cv.bytes();
+  return w;
+}
+
+int check_attn(const aj_attn_cfg *c, const aj_varlen *v, const char *name) {
+  AJ_REQUIRE(c && v, AJ_ERR_NULL, "%s: null cfg/varlen", name);
+  AJ_REQUIRE(c->dtype == AJ_F32 || c->dtype == AJ_BF16, AJ_ERR_UNSUPPORTED, "%s: dtype %d", name,
+             c->dtype);
+  AJ_REQUIRE(c->n_q_heads > 0 && c->n_kv_heads > 0 && c->n_q_heads % c->n_kv_heads == 0 &&
+                 c->n_q_heads <= 65535,
+             AJ_ERR_SHAPE, "%s: heads %d/%d", name, c->n_q_heads, c->n_kv_heads);
+  AJ_REQUIRE(c->head_dim >= 8 && c->head_dim <= kMaxHd && c->head_dim % 8 == 0,
+             AJ_ERR_UNSUPPORTED, "%s: head_dim %d (8..128, multiple of 8)", name, c->head_dim);
+  AJ_REQUIRE(c->window >= 0 && c->n_sink >= 0, AJ_ERR_SHAPE, "%s: window %d n_sink %d", name,
+             c->window, c->n_sink);
+  AJ_REQUIRE(c->scale >= 0.f && c->scale <= 3e38f, AJ_ERR_SHAPE, "%s: scale", name);
+  AJ_REQUIRE(v->n_tok >= 0 && v->n_seg >= 0 && (v->n_tok == 0 || v->n_seg > 0), AJ_ERR_SHAPE,
+             "%s: n_tok %d n_seg %d", name, v->n_tok, v->n_seg);
+  // rows are added to in 32 bits, and waves of one (row, head) counted in them
+  AJ_REQUIRE(v->n_tok <= 1 << 30 && (int64_t)v->n_tok * c->n_q_heads < (int64_t)1 << 32,
+             AJ_ERR_SHAPE, "%s: n_tok %d (at most 2^30) times %d heads (below 2^32)", name, v->n_tok,
+             c->n_q_heads);
+  AJ_REQUIRE(v->n_tok == 0 || v->cu_seqlens, AJ_ERR_NULL, "%s: null offsets", name);
+  return AJ_OK;
+}
+
+float attn_scale(const aj_attn_cfg &c) {
+  return c.scale > 0.f ? c.scale : 1.0f / sqrtf((float)c.head_dim);
+}
+
+}  // namespace
 }  // namespace aj
+
+extern "C" size_t aj_attention_workspace_bytes(const aj_attn_cfg *cfg, int32_t n_tok) {
+  if (!cfg || n_tok < 0 || cfg->n_q_heads <= 0 || cfg->n_kv_heads <= 0 || cfg->head_dim <= 0) return 0;
+  return aj::carve_attn(*cfg, n_tok, nullptr).bytes;
+}
+
+extern "C" int aj_attention_fwd(const aj_attn_cfg *cfg, const aj_varlen *vl, const void *qkv,
+                                void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+  const char *name = "aj_attention_fwd";
+  int r;
+  if ((r = aj::check_attn(cfg, vl, name))) return r;
+  if (vl->n_tok == 0) return AJ_OK;
+  AJ_REQUIRE(qkv && out && lse && ws, AJ_ERR_NULL, "%s: null pointer", name);
+  const aj::AttnWs w = aj::carve_attn(*cfg, vl->n_tok, ws);
+  AJ_REQUIRE(ws_bytes >= w.bytes, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes, w.bytes);
+  aj::AttnArgs a{vl->n_tok, vl->n_seg, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, vl->base,
+                 vl->cu_seqlens, qkv, out, lse, aj::attn_scale(*cfg)};
+  a.window = cfg->window;
+  a.n_sink = cfg->n_sink;
+  a.lse_log2 = true;
+  return cfg->dtype == AJ_BF16 ? aj::attn_fwd<bf16_t>(a, (hipStream_t)stream)
+                               : aj::attn_fwd<float>(a, (hipStream_t)stream);
+}
+
+extern "C" int aj_attention_bwd(const aj_attn_cfg *cfg, const aj_varlen *vl, const void *qkv,
+                                const void *out, const float *lse, const void *dout, void *dqkv,
+                                void *ws, size_t ws_bytes, void *stream) {
+  const char *name = "aj_attention_bwd";
+  int r;
+  if ((r = aj::check_attn(cfg, vl, name))) return r;
+  if (vl->n_tok == 0) return AJ_OK;
+  AJ_REQUIRE(qkv && out && lse && dout && dqkv && ws, AJ_ERR_NULL, "%s: null pointer", name);
+  const aj::AttnWs w = aj::carve_attn(*cfg, vl->n_tok, ws);
+  AJ_REQUIRE(ws_bytes >= w.bytes, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes, w.bytes);
+  aj::AttnBwdArgs a{vl->n_tok, vl->n_seg, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, vl->base,
+                    vl->cu_seqlens, qkv, out, dout, lse, w.delta, dqkv, aj::attn_scale(*cfg)};
+  a.window = cfg->window;
+  a.n_sink = cfg->n_sink;
+  a.lse_log2 = true;
+  a.part = w.part;
+  a.part_floats = w.part_floats;
+  return cfg->dtype == AJ_BF16 ? aj::attn_bwd<bf16_t>(a, (hipStream_t)stream)
+                               : aj::attn_bwd<float>(a, (hipStream_t)stream);
+}

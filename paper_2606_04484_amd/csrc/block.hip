@@ -213,6 +213,8 @@ int check_cfg(const aj_block_cfg *c, const char *name) {
              "%s: head_dim %d (8..128, multiple of 8)", name, c->head_dim);
   AJ_REQUIRE(c->d_ff > 0 && c->d_ff % 8 == 0, AJ_ERR_SHAPE, "%s: d_ff %d", name, c->d_ff);
   AJ_REQUIRE(c->rms_eps > 0 && c->rope_theta > 1, AJ_ERR_SHAPE, "%s: eps/theta", name);
+  AJ_REQUIRE(c->window >= 0 && c->n_sink >= 0, AJ_ERR_SHAPE, "%s: window %d n_sink %d", name,
+             c->window, c->n_sink);
   return AJ_OK;
 }
 
@@ -250,6 +252,8 @@ int block_fwd(const aj_block_cfg &c, const aj_block_weights &w, const aj_varlen 
   rope<T>((T *)sv.qkv, n, v.pos, Hq + Hkv, qdim, hd, c.rope_theta, false, st);
   AttnArgs at{n, v.n_seg, Hq, Hkv, hd, v.base, v.cu_seqlens, sv.qkv, sv.o, sv.lse,
               1.0f / sqrtf((float)hd)};
+  at.window = c.window;
+  at.n_sink = c.n_sink;
   if ((r = attn_fwd<T>(at, st))) return r;
   g = Gemm();
   g.M = n; g.N = d; g.K = Hq * hd;
@@ -350,6 +354,8 @@ int block_bwd(const aj_block_cfg &c, const aj_block_weights &w, const aj_varlen 
   if ((r = gemm<T>(g, st))) return r;
   AttnBwdArgs ab{n, v.n_seg, Hq, Hkv, hd, v.base, v.cu_seqlens, sv.qkv, sv.o, ws.dout, sv.lse,
                  ws.delta, ws.dqkv, 1.0f / sqrtf((float)hd)};
+  ab.window = c.window;
+  ab.n_sink = c.n_sink;
   if constexpr (sizeof(T) == 2) {   // d gate / d up has been read: scratch
     ab.part = (float *)ws.dgu;
     ab.part_floats = (size_t)n * F;

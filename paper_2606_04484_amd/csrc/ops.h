@@ -106,8 +106,12 @@ struct AttnArgs {
   const void *qkv;      // [n_tok, (Hq+2Hkv)*hd], q and k already rotated
   void *o;              // [n_tok, Hq*hd]
   float *lse;           // [Hq, n_tok] log-sum-exp of the scaled scores (log2 units on
-                        // the matrix-core path, natural log on the plain one)
+                        // the matrix-core path, natural log on the plain one unless
+                        // lse_log2)
   float scale;
+  int window = 0;       // > 0: a row sees its segment's keys in the last `window` rows
+  int n_sink = 0;       // and the segment's first n_sink ones
+  bool lse_log2 = false;
 };
 template <typename T>
 int attn_fwd(const AttnArgs &a, hipStream_t s);
@@ -123,9 +127,14 @@ struct AttnBwdArgs {
   float scale;
   float *part = nullptr;    // scratch for dK, dV in parts (16-byte aligned), part_floats of it
   size_t part_floats = 0;
+  int window = 0, n_sink = 0;   // as the forward's
+  bool lse_log2 = false;
 };
 template <typename T>
 int attn_bwd(const AttnBwdArgs &a, hipStream_t s);
+
+// Whether a window hides anything in a pack of n_tok rows.
+bool windowed(int window, int n_tok);
 
 // bfloat16 MFMA flash attention (head_dim 64 or 128, 16-byte aligned tensors)
 bool attn_mfma_supported(int hd, const void *p0, const void *p1, const void *p2);

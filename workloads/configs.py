@@ -31,6 +31,8 @@ class ModelConfig:
     vocab_chunk: int = 32768
     pack_tokens: int = 131072
     n_layers: int = 1            # decoder blocks between the embedding and the final norm
+    window: int = 0              # attention window in tokens (0: full causal attention)
+    n_sink: int = 0              # first tokens of a segment that stay visible past the window
 
     @property
     def qkv_dim(self) -> int:
