@@ -62,8 +62,9 @@ enum {
   AJ_DEVERR_BAD_FLAGS = 2,     /* author 3, or a timeline not starting a block */
   AJ_DEVERR_EMPTY = 4,         /* an empty timeline */
   AJ_DEVERR_OFFSETS = 8,       /* offsets not monotone, out of range, or not tiling [0, n) */
-  AJ_DEVERR_BLOCKS = 16        /* text-level merge: the block-start bits do not give n_blk
+  AJ_DEVERR_BLOCKS = 16,       /* text-level merge: the block-start bits do not give n_blk
                                   blocks, or a timeline does not start a block */
+  AJ_DEVERR_TOKEN_TWICE = 32   /* a token listed twice for one row */
 };
 
 const char *aj_status_str(int status);
@@ -483,6 +484,69 @@ int aj_logprob_pg_loss_bwd(const aj_loss_cfg *cfg, const aj_loss_in *in, const v
                            const float *logprob, const float *lse, float *dh,
                            float *d_final_norm, float *d_w_vocab, void *ws, size_t ws_bytes,
                            void *stream);
+
+/* ------------------------------------------------------------------ 3b. distillation
+ * Learning from a teacher's most probable tokens: a teacher scores a position
+ * and hands over its k largest log-probs; the student's loss at that position
+ * is the KL divergence from the teacher's distribution to its own.  These calls
+ * take rows of logits (the LM head's entry points below form them); each reads
+ * them once or, with the gradient, twice, and does all sums of a row over its
+ * parts in float32 and over the parts in 64 bits, in one fixed order
+ * (bit-identical on every call).
+ */
+typedef struct {
+  int32_t rows, vocab;          /* vocab at most 2^24 */
+  int64_t ld;                   /* elements from row to row, >= vocab; rows need no alignment */
+  int32_t dtype;                /* aj_dtype of the logits */
+  float inv_temp;               /* probabilities are softmax(logits * inv_temp); > 0 */
+  const void *logits;
+} aj_logits;
+
+/* The k largest logits of every row (1 <= k <= 256, k <= vocab), larger first, equal
+ * ones (-0 equals 0) by the lower index, NaN before all:
+ *   idx [rows, k] int32, logprob [rows, k] = logit * inv_temp - lse,
+ *   lse [rows] = log sum exp(logit * inv_temp) over the whole row (natural log).
+ * Logits of -inf have log-prob -inf (also where a row holds nothing else); a NaN or +inf
+ * makes its row's lse NaN.  ws: aj_topk_workspace_bytes for at least these rows. */
+size_t aj_topk_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
+int aj_topk_logprob(const aj_logits *lg, int32_t k, int32_t *idx, float *logprob, float *lse,
+                    void *ws, size_t ws_bytes, void *stream);
+
+/* A teacher's lists, one of k entries per row (1 <= k <= 256):
+ * idx < 0 marks an unused entry.  An idx >= vocab or a token listed again sets
+ * AJ_DEVERR_TOKEN_RANGE / AJ_DEVERR_TOKEN_TWICE in *err (err may be NULL), and the entry
+ * (of equal ones all but the first) counts as unused. */
+typedef struct {
+  int32_t k;
+  int32_t tail;                 /* 0: p = softmax of the listed log-probs, nothing outside;
+                                   1: p = exp(logprob), and what is left of 1 is one more
+                                   class, all tokens that are not listed */
+  const int32_t *idx;           /* [rows, k] */
+  const float *logprob;         /* [rows, k] natural log; -inf: probability 0 */
+  const float *weight;          /* [rows] weight of each row, or NULL for 1 */
+  float coef;                   /* of every row's gradient and share of stats */
+} aj_teacher;
+
+/* With q = softmax(logits * inv_temp), q_rest the sum of q over the tokens that are not
+ * listed and p_rest = max(0, 1 - sum p) (tail 1; 0 for tail 0):
+ *   loss[row] = sum_k p_k (log p_k - log q_k) + p_rest (log p_rest - log q_rest)
+ * (0 for a row with nothing listed; not scaled by weight or coef).  lse: [2, rows], the
+ * log-sum-exp of the row's logits * inv_temp and that of the tokens not listed; the
+ * backward reads it.  stats (may be NULL): float32[2] accumulated: [0] the sum of
+ * coef * weight * loss, [1] rows.  ws: aj_distill_workspace_bytes for at least these rows.
+ * The gradient, d logits [rows, vocab] in d_dtype with row stride ldd, is WRITTEN:
+ *   coef * weight * inv_temp * (M q_v - p_v),  M = sum p + p_rest,
+ * with p_v of a token that is not listed its share of p_rest, q_v / q_rest.  d logits may
+ * be the logits themselves (same type and ld), nothing else that overlaps them.
+ * fwd_bwd is both in one call. */
+size_t aj_distill_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
+int aj_distill_loss_fwd(const aj_logits *lg, const aj_teacher *t, float *loss, float *lse,
+                        float *stats, int32_t *err, void *ws, size_t ws_bytes, void *stream);
+int aj_distill_loss_bwd(const aj_logits *lg, const aj_teacher *t, const float *lse, void *dlogits,
+                        int64_t ldd, int32_t d_dtype, void *stream);
+int aj_distill_loss_fwd_bwd(const aj_logits *lg, const aj_teacher *t, float *loss, float *lse,
+                            float *stats, int32_t *err, void *dlogits, int64_t ldd, int32_t d_dtype,
+                            void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------ 4. around the update
  * GRPO advantages (Section 3: GRPO-style updates; groups of rollouts per

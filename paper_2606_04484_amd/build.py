@@ -14,7 +14,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libaj.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["status.cpp", "merge.hip", "ops.hip", "embed.hip", "gemm.hip", "attention.hip", "attention_mfma.hip", "block.hip",
-           "loss.hip", "update.hip", "ceiling.hip"]
+           "loss.hip", "logits.hip", "update.hip", "ceiling.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

@@ -112,6 +112,16 @@ class LossIn(C.Structure):
                 ("kl_coef", f32), ("w_vocab_t", vp)]
 
 
+class Logits(C.Structure):
+    _fields_ = [("rows", i32), ("vocab", i32), ("ld", i64), ("dtype", i32), ("inv_temp", f32),
+                ("logits", vp)]
+
+
+class Teacher(C.Structure):
+    _fields_ = [("k", i32), ("tail", i32), ("idx", vp), ("logprob", vp), ("weight", vp),
+                ("coef", f32)]
+
+
 EXPORTS = {
     "aj_status_str": (C.c_char_p, [C.c_int]),
     "aj_last_error": (C.c_char_p, []),
@@ -158,6 +168,14 @@ EXPORTS = {
                                          vp, vp, vp, vp, vp, sz, vp]),
     "aj_logprob_pg_loss_bwd": (C.c_int, [C.POINTER(LossCfg), C.POINTER(LossIn), vp, vp, vp, vp,
                                          vp, vp, vp, vp, vp, vp, sz, vp]),
+    "aj_topk_workspace_bytes": (sz, [i32, i32, i32]),
+    "aj_topk_logprob": (C.c_int, [C.POINTER(Logits), i32, vp, vp, vp, vp, sz, vp]),
+    "aj_distill_workspace_bytes": (sz, [i32, i32, i32]),
+    "aj_distill_loss_fwd": (C.c_int, [C.POINTER(Logits), C.POINTER(Teacher), vp, vp, vp, vp, vp,
+                                      sz, vp]),
+    "aj_distill_loss_bwd": (C.c_int, [C.POINTER(Logits), C.POINTER(Teacher), vp, vp, i64, i32, vp]),
+    "aj_distill_loss_fwd_bwd": (C.c_int, [C.POINTER(Logits), C.POINTER(Teacher), vp, vp, vp, vp,
+                                          vp, i64, i32, vp, sz, vp]),
     "aj_grpo_advantages": (C.c_int, [i32, vp, vp, f32, vp, vp, vp, vp]),
     "aj_select_workspace_bytes": (sz, [i32, i32]),
     "aj_select_episodes": (C.c_int, [C.POINTER(Timelines), vp, vp, C.POINTER(TimelinesOut), vp,
@@ -540,6 +558,103 @@ def aj_logprob_pg_loss_bwd(cfg, targets, tok, old_logprob, adv, inv_n_mask, h, f
                                         ptr(dh), ptr(d_final_norm), ptr(d_w_vocab), ptr(ws),
                                         ws.numel() * ws.element_size(), stream_handle(stream)),
            "aj_logprob_pg_loss_bwd")
+
+
+# ------------------------------------------------------------------ distillation
+
+def _rows_of(name, arg, t):
+    """(rows, vocab, ld, dtype code) of a matrix whose rows are each contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise AjError(f"{name}: {arg} must be a matrix")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise AjError(f"{name}: the rows of {arg} must be contiguous")
+    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1], dtype_code(t)
+
+
+def _logits(name, logits, inv_temp):
+    rows, vocab, ld, dt = _rows_of(name, "logits", logits)
+    return Logits(rows, vocab, ld, dt, inv_temp, ptr(logits))
+
+
+def aj_topk_workspace_bytes(rows, vocab, k):
+    return int(lib().aj_topk_workspace_bytes(int(rows), int(vocab), int(k)))
+
+
+def aj_topk_logprob(logits, inv_temp, idx, logprob, lse, ws, stream=None):
+    """idx int32, logprob float32 [rows, k]: the k largest of every row of logits under
+    softmax(logits * inv_temp); lse float32 [rows]."""
+    name = "aj_topk_logprob"
+    lg = _logits(name, logits, inv_temp)
+    if not isinstance(idx, torch.Tensor) or idx.dim() != 2:
+        raise AjError(f"{name}: idx must be a matrix")
+    k = idx.shape[1]
+    _operands(name, {"idx": (idx, (torch.int32,), (lg.rows, k)),
+                     "logprob": (logprob, (torch.float32,), (lg.rows, k)),
+                     "lse": (lse, (torch.float32,), (lg.rows,))})
+    _on_gpu(name, "logits", logits)
+    _check(lib().aj_topk_logprob(C.byref(lg), k, ptr(idx), ptr(logprob), ptr(lse),
+                                 *_workspace(name, ws), stream_handle(stream)), name)
+
+
+def teacher(idx, logprob, tail=False, weight=None, coef=1.0):
+    """A teacher's lists: idx int32 and logprob float32 [rows, k], weight float32 [rows] or
+    None; see aj_teacher.  Holds on to the tensors."""
+    t = Teacher(idx.shape[1] if idx.dim() == 2 else 0, 1 if tail else 0, ptr(idx), ptr(logprob),
+                ptr(weight), coef)
+    t.tensors = (idx, logprob, weight)
+    return t
+
+
+def _distill(name, logits, inv_temp, t, outs):
+    lg = _logits(name, logits, inv_temp)
+    idx, logprob, weight = t.tensors
+    f = (torch.float32,)
+    ops = {"idx": (idx, (torch.int32,), (lg.rows, t.k)), "logprob": (logprob, f, (lg.rows, t.k)),
+           "loss": (outs.get("loss"), f, (lg.rows,)), "lse": (outs.get("lse"), f, (2, lg.rows)),
+           "weight": (weight, f, (lg.rows,)), "stats": (outs.get("stats"), f, (2,)),
+           "err": (outs.get("err"), (torch.int32,), (1,))}
+    optional = {"weight", "stats", "err"} | ({"loss"} if "loss" not in outs else set())
+    _operands(name, {k: v for k, v in ops.items() if v[0] is not None or k not in optional})
+    _on_gpu(name, "logits", logits)
+    return lg
+
+
+def _dlogits(name, logits, dlogits):
+    rows, vocab, ld, dt = _rows_of(name, "dlogits", dlogits)
+    if dlogits.shape != logits.shape:
+        raise AjError(f"{name}: dlogits {tuple(dlogits.shape)} of logits {tuple(logits.shape)}")
+    _on_gpu(name, "dlogits", dlogits)
+    return ptr(dlogits), ld, dt
+
+
+def aj_distill_workspace_bytes(rows, vocab, k):
+    return int(lib().aj_distill_workspace_bytes(int(rows), int(vocab), int(k)))
+
+
+def aj_distill_loss_fwd(logits, inv_temp, t, loss, lse, ws, stats=None, err=None, stream=None):
+    """t: of teacher(); loss float32 [rows], lse float32 [2, rows]; stats: optional float32 [2]."""
+    name = "aj_distill_loss_fwd"
+    lg = _distill(name, logits, inv_temp, t, dict(loss=loss, lse=lse, stats=stats, err=err))
+    _check(lib().aj_distill_loss_fwd(C.byref(lg), C.byref(t), ptr(loss), ptr(lse), ptr(stats),
+                                     ptr(err), *_workspace(name, ws), stream_handle(stream)), name)
+
+
+def aj_distill_loss_bwd(logits, inv_temp, t, lse, dlogits, stream=None):
+    """dlogits: float32 or bfloat16, written; may be logits itself."""
+    name = "aj_distill_loss_bwd"
+    lg = _distill(name, logits, inv_temp, t, dict(lse=lse))
+    _check(lib().aj_distill_loss_bwd(C.byref(lg), C.byref(t), ptr(lse),
+                                     *_dlogits(name, logits, dlogits), stream_handle(stream)), name)
+
+
+def aj_distill_loss_fwd_bwd(logits, inv_temp, t, loss, lse, dlogits, ws, stats=None, err=None,
+                            stream=None):
+    """aj_distill_loss_fwd and _bwd in one call."""
+    name = "aj_distill_loss_fwd_bwd"
+    lg = _distill(name, logits, inv_temp, t, dict(loss=loss, lse=lse, stats=stats, err=err))
+    _check(lib().aj_distill_loss_fwd_bwd(C.byref(lg), C.byref(t), ptr(loss), ptr(lse), ptr(stats),
+                                         ptr(err), *_dlogits(name, logits, dlogits),
+                                         *_workspace(name, ws), stream_handle(stream)), name)
 
 
 # ------------------------------------------------------------------ around the update
