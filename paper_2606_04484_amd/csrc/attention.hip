@@ -212,7 +212,7 @@ AJ_DEV bool vec4(const void *p, int64_t ld, int es) {
 }
 
 template <typename T, int NC, bool WIN>
-__global__ __launch_bounds__(256) void attn_fwd_f32_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256) void attn_fwd_f32_kernel(WinAttnArgs a) {
   __shared__ __attribute__((aligned(16))) float Ks[kStep<NC> * kLd<NC>], Vs[kStep<NC> * kLd<NC>];
   const int hd = a.hd, ld = (a.Hq + 2 * a.Hkv) * hd;
   const int h = blockIdx.y, g = (h * a.Hkv) / a.Hq;
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256) void attn_fwd_f32_kernel(AttnArgs a) {
 
 // delta[h][row] = sum_d dO * O
 template <typename T>
-__global__ __launch_bounds__(256) void attn_delta_kernel(AttnBwdArgs a) {
+__global__ __launch_bounds__(256) void attn_delta_kernel(WinAttnBwdArgs a) {
   const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (idx >= (int64_t)a.n_tok * a.Hq) return;
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnBwdArgs a) {
 
 // dQ rows: dq = scale * sum_j P_j (dO.V_j - delta) K_j
 template <typename T, int NC, bool WIN>
-__global__ __launch_bounds__(256) void attn_dq_f32_kernel(AttnBwdArgs a) {
+__global__ __launch_bounds__(256) void attn_dq_f32_kernel(WinAttnBwdArgs a) {
   __shared__ __attribute__((aligned(16))) float Ks[kStep<NC> * kLd<NC>], Vs[kStep<NC> * kLd<NC>];
   const int hd = a.hd, ld = (a.Hq + 2 * a.Hkv) * hd;
   const int h = blockIdx.y, g = (h * a.Hkv) / a.Hq;
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(AttnBwdArgs a) {
 // queries of the same segment at or after the key (with a window: the W of them
 // from the key on, all of them for a sink).
 template <typename T, int NC, bool WIN>
-__global__ __launch_bounds__(256) void attn_dkv_f32_kernel(AttnBwdArgs a) {
+__global__ __launch_bounds__(256) void attn_dkv_f32_kernel(WinAttnBwdArgs a) {
   __shared__ __attribute__((aligned(16))) float Qs[kStep<NC> * kLd<NC>], Ds[kStep<NC> * kLd<NC>];
   __shared__ __attribute__((aligned(16))) float Ls[kStep<NC>], Dl[kStep<NC>];
   const int hd = a.hd, ld = (a.Hq + 2 * a.Hkv) * hd;
@@ -490,13 +490,13 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(AttnBwdArgs a) {
 bool windowed(int window, int n_tok) { return window > 0 && window < n_tok; }
 
 template <typename T>
-int attn_fwd(const AttnArgs &args, hipStream_t s) {
-  AttnArgs a = args;
+int attn_fwd(const WinAttnArgs &args, hipStream_t s) {
+  WinAttnArgs a = args;
   if (a.n_tok <= 0) return AJ_OK;
   a.n_sink = std::min(a.n_sink, a.n_tok);   // the sums of rows stay in 32 bits
   if (a.hd > kMaxHd || a.hd % 8) return fail(AJ_ERR_UNSUPPORTED, "attention: head_dim %d", a.hd);
   const bool win = windowed(a.window, a.n_tok);
-  if (!win && sizeof(T) == 2 && attn_mfma_supported(a.hd, a.qkv, a.o, a.o)) return attn_fwd_mfma(a, s);
+  if (sizeof(T) == 2 && attn_mfma_supported(a.hd, a.qkv, a.o, a.o)) return attn_fwd_mfma(a, s);
   dim3 grid((a.n_tok + kRows - 1) / kRows, a.Hq);
   const int tk = timing_begin(s, AJ_KC_ATTN_FWD, 0.0);
   if (win) AJ_NC_DISPATCH(a.hd, (attn_fwd_f32_kernel<T, NC, true><<<grid, 256, 0, s>>>(a)));
@@ -506,8 +506,8 @@ int attn_fwd(const AttnArgs &args, hipStream_t s) {
 }
 
 template <typename T>
-int attn_bwd(const AttnBwdArgs &args, hipStream_t s) {
-  AttnBwdArgs a = args;
+int attn_bwd(const WinAttnBwdArgs &args, hipStream_t s) {
+  WinAttnBwdArgs a = args;
   if (a.n_tok <= 0) return AJ_OK;
   a.n_sink = std::min(a.n_sink, a.n_tok);
   if (a.hd > kMaxHd || a.hd % 8) return fail(AJ_ERR_UNSUPPORTED, "attention: head_dim %d", a.hd);
@@ -515,7 +515,7 @@ int attn_bwd(const AttnBwdArgs &args, hipStream_t s) {
   // the matrix-core forward saves its log-sum-exp in log2 units, the plain
   // kernels in natural ones unless asked for log2: the backward must then take the
   // forward's path
-  const bool fwd_mfma = !win && sizeof(T) == 2 && attn_mfma_supported(a.hd, a.qkv, a.o, a.o);
+  const bool fwd_mfma = sizeof(T) == 2 && attn_mfma_supported(a.hd, a.qkv, a.o, a.o);
   const bool bwd_mfma = fwd_mfma && attn_mfma_supported(a.hd, a.qkv, a.dout, a.dqkv);
   if (bwd_mfma) return attn_bwd_mfma(a, s);
   if (fwd_mfma && !a.lse_log2)
@@ -535,15 +535,22 @@ int attn_bwd(const AttnBwdArgs &args, hipStream_t s) {
   return check_launch("attention backward");
 }
 
+template <typename T> int attn_fwd(const AttnArgs &a, hipStream_t s) { return attn_fwd<T>(WinAttnArgs(a), s); }
+template <typename T> int attn_bwd(const AttnBwdArgs &a, hipStream_t s) { return attn_bwd<T>(WinAttnBwdArgs(a), s); }
+
 template int attn_fwd<float>(const AttnArgs &, hipStream_t);
 template int attn_fwd<bf16_t>(const AttnArgs &, hipStream_t);
 template int attn_bwd<float>(const AttnBwdArgs &, hipStream_t);
 template int attn_bwd<bf16_t>(const AttnBwdArgs &, hipStream_t);
+template int attn_fwd<float>(const WinAttnArgs &, hipStream_t);
+template int attn_fwd<bf16_t>(const WinAttnArgs &, hipStream_t);
+template int attn_bwd<float>(const WinAttnBwdArgs &, hipStream_t);
+template int attn_bwd<bf16_t>(const WinAttnBwdArgs &, hipStream_t);
 
 namespace {
 
 struct AttnWs {
-  float *delta, *part;
+  float *delta, *part, *sink;
   size_t part_floats, bytes;
 };
 
@@ -557,6 +564,7 @@ AttnWs carve_attn(const aj_attn_cfg &c, int n, void *base) {
   if (c.dtype == AJ_BF16)
     w.part_floats = std::min((size_t)2 * c.n_q_heads * n * c.head_dim, (size_t)64 << 20);
   w.part = cv.take<float>(w.part_floats);
+  w.sink = cv.take<float>(c.dtype == AJ_BF16 ? attn_sink_floats(c.window, c.n_sink, n, c.n_q_heads, c.head_dim) : 0);
   w.bytes = cv.bytes();
   return w;
 }
@@ -604,8 +612,8 @@ extern "C" int aj_attention_fwd(const aj_attn_cfg *cfg, const aj_varlen *vl, con
   AJ_REQUIRE(qkv && out && lse && ws, AJ_ERR_NULL, "%s: null pointer", name);
   const aj::AttnWs w = aj::carve_attn(*cfg, vl->n_tok, ws);
   AJ_REQUIRE(ws_bytes >= w.bytes, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes, w.bytes);
-  aj::AttnArgs a{vl->n_tok, vl->n_seg, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, vl->base,
-                 vl->cu_seqlens, qkv, out, lse, aj::attn_scale(*cfg)};
+  aj::WinAttnArgs a(aj::AttnArgs{vl->n_tok, vl->n_seg, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim,
+                                 vl->base, vl->cu_seqlens, qkv, out, lse, aj::attn_scale(*cfg)});
   a.window = cfg->window;
   a.n_sink = cfg->n_sink;
   a.lse_log2 = true;
@@ -623,13 +631,15 @@ extern "C" int aj_attention_bwd(const aj_attn_cfg *cfg, const aj_varlen *vl, con
   AJ_REQUIRE(qkv && out && lse && dout && dqkv && ws, AJ_ERR_NULL, "%s: null pointer", name);
   const aj::AttnWs w = aj::carve_attn(*cfg, vl->n_tok, ws);
   AJ_REQUIRE(ws_bytes >= w.bytes, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes, w.bytes);
-  aj::AttnBwdArgs a{vl->n_tok, vl->n_seg, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, vl->base,
-                    vl->cu_seqlens, qkv, out, dout, lse, w.delta, dqkv, aj::attn_scale(*cfg)};
+  aj::WinAttnBwdArgs a(aj::AttnBwdArgs{vl->n_tok, vl->n_seg, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim,
+                                       vl->base, vl->cu_seqlens, qkv, out, dout, lse, w.delta, dqkv,
+                                       aj::attn_scale(*cfg)});
   a.window = cfg->window;
   a.n_sink = cfg->n_sink;
   a.lse_log2 = true;
   a.part = w.part;
   a.part_floats = w.part_floats;
+  a.sink_part = w.sink;
   return cfg->dtype == AJ_BF16 ? aj::attn_bwd<bf16_t>(a, (hipStream_t)stream)
                                : aj::attn_bwd<float>(a, (hipStream_t)stream);
 }

@@ -73,11 +73,75 @@ template <typename A> AJ_DEV int seg_end(const A &a, int row) {
 // multiple of 8 every tile of a head still runs on one XCD.
 AJ_DEV int work_item(int wg) { return wg; }
 
-AJ_DEV float wave_min_f(float v) {
+constexpr int kTR = 64;       // token rows per staged tile
+
+AJ_DEV int wave_min(int v) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fminf(v, __shfl_xor(v, o, 64));
+  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
   return v;
 }
+AJ_DEV int wave_max(int v) { return -wave_min(-v); }
+
+// The key tiles of a workgroup of query rows from q0 to hi.  Without a window: those of
+// [segment start of q0, hi].  With one: those of [lo, hi], lo the first key in
+// q0's window (which takes in the sinks of the segments that start in between), and
+// before them those of the sinks [s0, s0 + n_sink) of q0's segment that lie below lo.
+template <bool WIN>
+struct KeyTiles {
+  int lo, hi, s0, s1, n_sink, n;    // s1: one past the sinks below lo; n_sink, n: tiles
+  template <typename A> AJ_DEV void init(const A &a, int q0, int rows) {
+    hi = min(q0 + rows - 1, a.n_tok - 1);
+    lo = s0 = s1 = seg_start(a, q0);
+    if (WIN) {
+      lo = max(s0, q0 - a.window + 1);
+      s1 = s0 + min(a.n_sink, lo - s0);
+    }
+    n_sink = (s1 - s0 + kTR - 1) / kTR;
+    n = n_sink + (hi - lo + kTR) / kTR;
+  }
+  // the same values in scalar registers (every lane has read the same ones)
+  AJ_DEV void uniform() {
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    s0 = __builtin_amdgcn_readfirstlane(s0);
+    s1 = __builtin_amdgcn_readfirstlane(s1);
+    n_sink = __builtin_amdgcn_readfirstlane(n_sink);
+    n = __builtin_amdgcn_readfirstlane(n);
+  }
+  AJ_DEV bool sinks(int it) const { return WIN && it < n_sink; }
+  AJ_DEV int first(int it) const {
+    return WIN ? (it < n_sink ? s0 + it * kTR : lo + (it - n_sink) * kTR) : lo + it * kTR;
+  }
+  AJ_DEV int rows(int it) const { return sinks(it) ? s1 : hi + 1; }
+};
+
+// What a lane's query row q (of a segment that starts at qs) sees of a key tile: keys
+// k0 + 4 hl + off with off in [lo, hi], or, of a tile that is not the sinks' own, with
+// (unsigned)(off - slo) < ns.
+struct Seen {
+  int lo, hi, slo;
+  uint32_t ns;
+  template <bool WIN>
+  AJ_DEV Seen(const KeyTiles<WIN> &kt, int it, int k0, int q, int qs, int low, int n_sink, int hl) {
+    const int b = k0 + 4 * hl;
+    lo = low - b;
+    hi = q - b;
+    slo = qs - b;
+    ns = 0;
+    if (WIN) {
+      if (kt.sinks(it)) {
+        lo = slo;
+        hi = kt.s1 - 1 - b;
+      } else {
+        // those from `low` on are in [lo, hi] already
+        ns = min(n_sink, low - qs);
+      }
+    }
+  }
+  template <bool WIN> AJ_DEV bool has(int off) const {
+    return WIN ? (off >= lo & off <= hi) | ((uint32_t)(off - slo) < ns) : off >= lo && off <= hi;
+  }
+};
 
 // ------------------------------------------------------------------ LDS tiles
 // A tile of 64 token rows x HD bfloat16, row-major in LDS (HD*2 bytes per
@@ -96,7 +160,6 @@ AJ_DEV float wave_min_f(float v) {
 //   HD = 64 (two rows a line):  swz(r) = 2*((r >> 1) & 3) | ((r >> 3) & 1)
 // (bijective on 16 consecutive rows; within an aligned group of 4 rows the
 // values differ in a bit other than bit 0, so chunks c and c^1 never meet).
-constexpr int kTR = 64;       // token rows per staged tile
 
 AJ_DEV uint32_t lds_addr(const void *p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
@@ -354,13 +417,13 @@ AJ_DEV void cols_times_half(f32x16_t (&acc)[HD / 32], const TileLanes<HD> &L, co
 // ------------------------------------------------------------------ forward
 // One workgroup: 32 * NW queries of one head (NW waves of 32), key tiles of 64
 // double-buffered and shared by all the waves; a lane owns one query.
-template <int HD, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_fwd_mfma_kernel(AttnArgs a, int n_qt) {
+template <int HD, int NW, bool WIN>
+__global__ __launch_bounds__(64 * NW, 2) void attn_fwd_mfma_kernel(WinAttnArgs a, int n_qt) {
   using TT = TokTile<HD, NW>;
   constexpr int KS = HD / 16, DT = HD / 32, T = TT::kBytes;
   // two stages of a K and a V tile: K at 0 and T, V at 2T and 3T (bytes)
   __shared__ __attribute__((aligned(16))) uint16_t sm[4 * TT::kHalfs];
-  __shared__ int rng[2];
+  __shared__ KeyTiles<WIN> shared_tiles;
   TileLanes<HD> L;
   L.init(sm);
   const int t = work_item(blockIdx.x);
@@ -373,10 +436,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_mfma_kernel(AttnArgs a, i
   const bool qv = q < a.n_tok;
   const int qs = qv ? seg_start(a, q) : a.n_tok;
   const bf16_t *qkv = (const bf16_t *)a.qkv;
-  if (threadIdx.x == 0) {
-    rng[0] = seg_start(a, q0);
-    rng[1] = min(q0 + 32 * NW - 1, a.n_tok - 1);
-  }
+  // the first key of the row's window
+  const int low = WIN ? max(qs, q - a.window + 1) : qs;
+  if (threadIdx.x == 0) shared_tiles.init(a, q0, 32 * NW);
   bf16x8_t qf[KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
@@ -391,42 +453,44 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_mfma_kernel(AttnArgs a, i
     for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
   float m = -INFINITY, lsum = 0.f;
   const float c = a.scale * kLog2e;
-  const int w_lo = (int)wave_min_f((float)qs);          // earliest key any row of the wave reads
   const int w_hi = min(q0 + 32 * w + 31, a.n_tok - 1);   // latest query row of the wave
-  const int w_qs = (int)-wave_min_f(-(float)qs);        // latest segment start of the wave
+  const int w_low = wave_max(low);        // from here on every row of the wave sees keys up to its own
   __syncthreads();
-  const int kv_lo = rng[0], kv_hi = rng[1];
-  const int n_kt = (kv_hi - kv_lo + kTR) / kTR;
+  KeyTiles<WIN> kt = shared_tiles;
+  if (WIN) kt.uniform();
+  // earliest key any row of the wave reads, past the sinks' own tiles; whether any reads those
+  const int w_lo = wave_min(WIN && a.n_sink > 0 && qs + a.n_sink > kt.lo ? max(qs, kt.lo) : low);
+  const bool w_sinks = WIN && __builtin_amdgcn_ballot_w64(qs == kt.s0);
   const bf16_t *kbase = qkv + (a.Hq + g) * HD, *vbase = qkv + (a.Hq + a.Hkv + g) * HD;
-  TT::load(sm, kbase, ld, kv_lo, kv_hi + 1);
-  TT::load(sm + 2 * TT::kHalfs, vbase, ld, kv_lo, kv_hi + 1);
+  TT::load(sm, kbase, ld, kt.first(0), kt.rows(0));
+  TT::load(sm + 2 * TT::kHalfs, vbase, ld, kt.first(0), kt.rows(0));
   dma_wait();
   __syncthreads();
   // tile it reads stage st and prefetches tile it + 1 into the other stage;
   // the loop runs two tiles per pass so that both stages are fixed offsets
   auto tile = [&](const int it, const int st) __attribute__((always_inline)) {
-    const int k0 = kv_lo + it * kTR;
-    if (it + 1 < n_kt) {
-      TT::load(sm + (st ^ 1) * TT::kHalfs, kbase, ld, k0 + kTR, kv_hi + 1);
-      TT::load(sm + (2 + (st ^ 1)) * TT::kHalfs, vbase, ld, k0 + kTR, kv_hi + 1);
+    const int k0 = kt.first(it);
+    if (it + 1 < kt.n) {
+      TT::load(sm + (st ^ 1) * TT::kHalfs, kbase, ld, kt.first(it + 1), kt.rows(it + 1));
+      TT::load(sm + (2 + (st ^ 1)) * TT::kHalfs, vbase, ld, kt.first(it + 1), kt.rows(it + 1));
     }
-    if (k0 <= w_hi && k0 + kTR - 1 >= w_lo) {
+    if (kt.sinks(it) ? w_sinks : k0 <= w_hi && k0 + kTR - 1 >= w_lo) {
       f32x16_t s[2];
       rows_times<HD, true>(s, L, st * T, qf);            // S^T = K Q^T (unscaled)
       float mx = -INFINITY;
-      if (k0 >= w_qs && k0 + kTR - 1 <= q0 + 32 * w) {   // every key visible to every row
+      if (!kt.sinks(it) && k0 >= w_low && k0 + kTR - 1 <= q0 + 32 * w) {   // every key visible to every row
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
           for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[tt][r]);
       } else {
-        const int lo = qs - k0 - 4 * hl, hi = q - k0 - 4 * hl;
+        const Seen seen(kt, it, k0, q, qs, low, a.n_sink, hl);
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int off = 32 * tt + 8 * (r >> 2) + (r & 3);
-            s[tt][r] = (off >= lo && off <= hi) ? s[tt][r] : -INFINITY;
+            s[tt][r] = seen.template has<WIN>(off) ? s[tt][r] : -INFINITY;
             mx = fmaxf(mx, s[tt][r]);
           }
       }
@@ -467,9 +531,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_mfma_kernel(AttnArgs a, i
     dma_wait();
     __syncthreads();
   };
-  for (int it = 0; it < n_kt; it += 2) {
+  for (int it = 0; it < kt.n; it += 2) {
     tile(it, 0);
-    if (it + 1 < n_kt) tile(it + 1, 1);
+    if (it + 1 < kt.n) tile(it + 1, 1);
   }
   lsum += __shfl_xor(lsum, 32, 64);
   if (!qv) return;
@@ -490,13 +554,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_mfma_kernel(AttnArgs a, i
 
 // ------------------------------------------------------------------ dQ
 // Same workgroup shape as the forward; a lane owns one query.
-template <int HD, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(AttnBwdArgs a, int n_qt) {
+template <int HD, int NW, bool WIN>
+__global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(WinAttnBwdArgs a, int n_qt) {
   using TT = TokTile<HD, NW>;
   constexpr int KS = HD / 16, DT = HD / 32, T = TT::kBytes;
   // two stages of a K and a V tile: K at 0 and T, V at 2T and 3T (bytes)
   __shared__ __attribute__((aligned(16))) uint16_t sm[4 * TT::kHalfs];
-  __shared__ int rng[2];
+  __shared__ KeyTiles<WIN> shared_tiles;
   TileLanes<HD> L;
   L.init(sm);
   const int t = work_item(blockIdx.x);
@@ -510,10 +574,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(AttnBwdArgs a,
   const int qs = qv ? seg_start(a, q) : a.n_tok;
   const bf16_t *qkv = (const bf16_t *)a.qkv;
   const bf16_t *dout = (const bf16_t *)a.dout;
-  if (threadIdx.x == 0) {
-    rng[0] = seg_start(a, q0);
-    rng[1] = min(q0 + 32 * NW - 1, a.n_tok - 1);
-  }
+  // the first key of the row's window
+  const int low = WIN ? max(qs, q - a.window + 1) : qs;
+  if (threadIdx.x == 0) shared_tiles.init(a, q0, 32 * NW);
   bf16x8_t qf[KS], df[KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
@@ -545,20 +608,22 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(AttnBwdArgs a,
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
   const float c = a.scale * kLog2e;
-  const int w_lo = (int)wave_min_f((float)qs);
   const int w_hi = min(q0 + 32 * w + 31, a.n_tok - 1);
-  const int w_qs = (int)-wave_min_f(-(float)qs);        // latest segment start of the wave
+  const int w_low = wave_max(low);        // from here on every row of the wave sees keys up to its own
   __syncthreads();
-  const int kv_lo = rng[0], kv_hi = rng[1];
-  const int n_kt = (kv_hi - kv_lo + kTR) / kTR;
+  KeyTiles<WIN> kt = shared_tiles;
+  if (WIN) kt.uniform();
+  // earliest key any row of the wave reads, past the sinks' own tiles; whether any reads those
+  const int w_lo = wave_min(WIN && a.n_sink > 0 && qs + a.n_sink > kt.lo ? max(qs, kt.lo) : low);
+  const bool w_sinks = WIN && __builtin_amdgcn_ballot_w64(qs == kt.s0);
   const bf16_t *kbase = qkv + (a.Hq + g) * HD, *vbase = qkv + (a.Hq + a.Hkv + g) * HD;
-  TT::load(sm, kbase, ld, kv_lo, kv_hi + 1);
-  TT::load(sm + 2 * TT::kHalfs, vbase, ld, kv_lo, kv_hi + 1);
+  TT::load(sm, kbase, ld, kt.first(0), kt.rows(0));
+  TT::load(sm + 2 * TT::kHalfs, vbase, ld, kt.first(0), kt.rows(0));
   dma_wait();
   __syncthreads();
   // key rows 32tt..32tt+31 of the tile at stage st: S^T = K Q^T, dP^T =
   // V dO^T, the softmax terms, then dQ^T += K^T dS^T over those 32 keys
-  auto half = [&](const int tt, const int st, const int k0,
+  auto half = [&](const int tt, const int st, const int it, const int k0,
                   const bool full) __attribute__((always_inline)) {
     f32x16_t s, dp;   // S^T and dP^T - delta, set by rows_times_pair
     if constexpr (!kSpread) {
@@ -571,13 +636,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(AttnBwdArgs a,
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = fast_exp2(fmaf(s[r], c, -lse2)) * dp[r];
     } else {
-      // key k0 + 4hl + off (off a constant per element) is visible iff
-      // lo <= off <= hi
-      const int lo = qs - k0 - 4 * hl, hi = q - k0 - 4 * hl;
+      const Seen seen(kt, it, k0, q, qs, low, a.n_sink, hl);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int off = 32 * tt + 8 * (r >> 2) + (r & 3);
-        const float p = (off >= lo && off <= hi) ? fast_exp2(fmaf(s[r], c, -lse2)) : 0.f;
+        const float p = seen.template has<WIN>(off) ? fast_exp2(fmaf(s[r], c, -lse2)) : 0.f;
         s[r] = p * dp[r];
       }
     }
@@ -587,23 +650,23 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(AttnBwdArgs a,
   // tile it reads stage st and prefetches tile it + 1 into the other stage;
   // two tiles per pass so that both stages are fixed offsets
   auto tile = [&](const int it, const int st) __attribute__((always_inline)) {
-    const int k0 = kv_lo + it * kTR;
-    if (it + 1 < n_kt) {
-      TT::load(sm + (st ^ 1) * TT::kHalfs, kbase, ld, k0 + kTR, kv_hi + 1);
-      TT::load(sm + (2 + (st ^ 1)) * TT::kHalfs, vbase, ld, k0 + kTR, kv_hi + 1);
+    const int k0 = kt.first(it);
+    if (it + 1 < kt.n) {
+      TT::load(sm + (st ^ 1) * TT::kHalfs, kbase, ld, kt.first(it + 1), kt.rows(it + 1));
+      TT::load(sm + (2 + (st ^ 1)) * TT::kHalfs, vbase, ld, kt.first(it + 1), kt.rows(it + 1));
     }
-    if (k0 <= w_hi && k0 + kTR - 1 >= w_lo) {
-      const bool full = k0 >= w_qs && k0 + kTR - 1 <= q0 + 32 * w;   // every key visible to every row
-      half(0, st, k0, full);
-      half(1, st, k0, full);
+    if (kt.sinks(it) ? w_sinks : k0 <= w_hi && k0 + kTR - 1 >= w_lo) {
+      const bool full = !kt.sinks(it) && k0 >= w_low && k0 + kTR - 1 <= q0 + 32 * w;   // every key visible to every row
+      half(0, st, it, k0, full);
+      half(1, st, it, k0, full);
     }
     lds_wait();
     dma_wait();
     __syncthreads();
   };
-  for (int it = 0; it < n_kt; it += 2) {
+  for (int it = 0; it < kt.n; it += 2) {
     tile(it, 0);
-    if (it + 1 < n_kt) tile(it + 1, 1);
+    if (it + 1 < kt.n) tile(it + 1, 1);
   }
   if (!qv) return;
   bf16_t *out = (bf16_t *)a.dqkv + (int64_t)q * ld + h * HD;
@@ -705,8 +768,28 @@ struct DkvSched {
   }
 };
 
-template <int HD, int NW>
-__global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, int parts) {
+// The keys of a window pass: a key sees the W queries from itself on, and a sink all of
+// its segment's.  Left at that, the workgroup of a long segment's first keys would walk
+// every query of it while the others walk W: where that is a longer way than
+// kSinkChunk, the sinks that see past their window ("far") get no query in the window
+// pass and a pass of their own, cut into chunks of kSinkChunk queries (and, like any dK/dV
+// work, query heads); a last kernel adds the chunks' float32 sums in order.  Chunk c of a
+// segment that starts at row s is number 2 floor(s / kSinkChunk) + c: such segments are
+// longer than kSinkChunk, so that their numbers never meet.
+constexpr int kSinkChunk = 1024;
+constexpr int kFarSinks = 128;     // most sinks that the far pass takes (one tile of keys)
+
+// rows of a chunk's sums
+__host__ AJ_DEV int far_rows(const WinAttnBwdArgs &a) { return a.n_sink; }
+AJ_DEV int far_sinks(const WinAttnBwdArgs &a, int seg_len) {
+  if (a.sink_part == nullptr || seg_len <= max(a.window, kSinkChunk)) return 0;
+  return min(a.n_sink, seg_len - a.window);
+}
+
+enum { kCausal, kWindow, kFar };
+
+template <int HD, int NW, int MODE>
+__global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a, int parts) {
   using TT = TokTile<HD, NW>;
   constexpr int KS = HD / 16, DT = HD / 32, T = TT::kBytes, RB = HD * 2;
   constexpr int NS = 8 * DT, NC = NS / 2, D = 3;
@@ -717,7 +800,7 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, i
   __shared__ __attribute__((aligned(16))) uint16_t smq[3 * TT::kHalfs];
   __shared__ __attribute__((aligned(16))) uint16_t smd[3 * TT::kHalfs];
   __shared__ __attribute__((aligned(16))) float ld_sm[6][kTR];
-  __shared__ int rng[1];
+  __shared__ int rng[NW];
   TileLanes<HD> LQ, LD;
   LQ.init(smq);
   LD.init(smd);
@@ -727,13 +810,38 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, i
   const int ld = (a.Hq + 2 * a.Hkv) * HD;
   const int ldo = a.Hq * HD;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, hl = lane >> 5, lq = lane & 31;
-  const int k0 = kt * 32 * NW;
+  int k0 = kt * 32 * NW;        // (kFar: kt is the number of a chunk)
+  int qt0 = k0;                 // the first query tile's first row
+  int far_hi = 0, n_far = 0;    // kFar: the chunk's last query, the segment's far sinks
+  if constexpr (MODE == kFar) {
+    const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, kt / 2 * kSinkChunk + kSinkChunk - 1);
+    const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
+    const int chunk = kt - s0 / kSinkChunk * 2;
+    if (s0 < 0 || chunk < 0) return;
+    n_far = far_sinks(a, s1 - s0);
+    if (n_far == 0 || chunk * kSinkChunk >= s1 - s0) return;
+    k0 = s0;
+    qt0 = s0 + chunk * kSinkChunk;
+    far_hi = min(qt0 + kSinkChunk, s1);
+  }
   const int kv = k0 + 32 * w + lq;            // the key row this lane owns
-  const bool kvv = kv < a.n_tok;
-  const int ke = kvv ? seg_end(a, kv) : 0;    // queries of the key: [kv, ke)
+  const bool kvv = MODE == kFar ? kv < k0 + n_far : kv < a.n_tok;
+  int ke = kvv ? MODE == kFar ? far_hi : seg_end(a, kv) : 0;    // queries of the key: [kv, ke)
+  if constexpr (MODE == kWindow) {
+    if (kvv && ke - kv > a.window) {
+      const int s0 = seg_start(a, kv);
+      if (kv - s0 >= a.n_sink) ke = kv + a.window;
+      else if (kv - s0 < far_sinks(a, ke - s0)) ke = kv;
+    }
+  }
   const bf16_t *qkv = (const bf16_t *)a.qkv;
   const bf16_t *dout = (const bf16_t *)a.dout;
-  if (threadIdx.x == 0) rng[0] = seg_end(a, min(k0 + 32 * NW - 1, a.n_tok - 1));
+  if constexpr (MODE == kWindow) {
+    const int hi = wave_max(ke);
+    if (lane == 0) rng[w] = hi;
+  } else if (threadIdx.x == 0) {
+    rng[0] = MODE == kFar ? far_hi : seg_end(a, min(k0 + 32 * NW - 1, a.n_tok - 1));
+  }
   bf16x8_t kf[KS], vf[KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
@@ -765,16 +873,21 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, i
     }
   }
   __syncthreads();
-  const int q_hi = rng[0];    // queries [k0, q_hi)
+  int q_hi = rng[0];          // queries [qt0, q_hi)
+  if constexpr (MODE == kWindow) {
+#pragma unroll
+    for (int i = 1; i < NW; ++i) q_hi = max(q_hi, rng[i]);
+  }
+  if constexpr (MODE != kCausal) q_hi = __builtin_amdgcn_readfirstlane(q_hi);
   // the part's query heads [h0, h0 + n_h) of the group
   const int group = a.Hq / a.Hkv, h_lo = group * part / parts, n_h = group * (part + 1) / parts - h_lo;
   const int h0 = g * group + h_lo;
-  const int n_qb = q_hi > k0 ? (q_hi - k0 + kTR - 1) / kTR : 0;
+  const int n_qb = q_hi > qt0 ? (q_hi - qt0 + kTR - 1) / kTR : 0;
   const int n_it = n_h * n_qb;
-  // item it: query head h0 + it / n_qb, query tile k0 + 64 * (it % n_qb)
+  // item it: query head h0 + it / n_qb, query tile qt0 + 64 * (it % n_qb)
   auto load_item = [&](int it, auto ST) __attribute__((always_inline)) {
     constexpr int st = decltype(ST)::value;
-    const int h = h0 + it / n_qb, qb = k0 + kTR * (it % n_qb);
+    const int h = h0 + it / n_qb, qb = qt0 + kTR * (it % n_qb);
     TT::load(smq + st * TT::kHalfs, qkv + h * HD, ld, qb, q_hi);
     TT::load(smd + st * TT::kHalfs, dout + h * HD, ldo, qb, q_hi);
     if (w < 2) {                // one float per lane: LSE (wave 0), delta (wave 1)
@@ -950,8 +1063,8 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, i
   auto item = [&](const int it, auto ST) __attribute__((always_inline)) {
     constexpr int st = decltype(ST)::value;
     // half tt of item i: row offset o is seen iff o - (lo(i) - 32tt) < span(i)
-    const int lo = kv - (k0 + kTR * (min(it, n_it - 1) % n_qb)) - 4 * hl;
-    const int lo1 = kv - (k0 + kTR * (min(it + 1, n_it - 1) % n_qb)) - 4 * hl;
+    const int lo = kv - (qt0 + kTR * (min(it, n_it - 1) % n_qb)) - 4 * hl;
+    const int lo1 = kv - (qt0 + kTR * (min(it + 1, n_it - 1) % n_qb)) - 4 * hl;
     step(Ci<1>{}, Ci<(st + 2) % 3>{}, Ci<0>{}, Ci<st>{}, Ci<1>{}, Ci<st>{}, Ci<0>{}, lo - 32,
          it < n_it ? span : 0, [] {});
     step(Ci<0>{}, Ci<st>{}, Ci<1>{}, Ci<st>{}, Ci<0>{}, Ci<(st + 1) % 3>{}, Ci<1>{}, lo1,
@@ -979,7 +1092,7 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, i
     dma_wait();
     __syncthreads();
     // LSE and delta, then S and dP - delta of half 0
-    const bool whole0 = seen_whole(kv - k0 - 4 * hl, span);
+    const bool whole0 = seen_whole(kv - qt0 - 4 * hl, span);
     read_ld(0, 0);
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
@@ -991,7 +1104,7 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, i
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) asm volatile("" : "+v"(dl[r4]));
       }
-      s = kk == 0 ? s_first(fq, whole0, kv - k0 - 4 * hl, span) : mfma(fq, kf[kk], s);
+      s = kk == 0 ? s_first(fq, whole0, kv - qt0 - 4 * hl, span) : mfma(fq, kf[kk], s);
       dp = mfma(fd, vf[kk], kk == 0 ? delta_init() : dp);
     }
     // the first step's dV/dK group: half -1 (stage 2, cleared)
@@ -1005,8 +1118,10 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, i
     tail(Ci<2>{});
   }
   if (!kvv) return;
-  if (parts > 1) {   // float32 sums of the part's heads, for attn_dkv_parts_kernel
-    float *p = a.part + ((int64_t)part * a.n_tok + kv) * (2 * a.Hkv * HD) + g * HD;
+  if (MODE == kFar || parts > 1) {   // float32 sums of the part's heads, added up by the kernels below
+    float *p = MODE == kFar
+                   ? a.sink_part + (((int64_t)kt * parts + part) * far_rows(a) + kv - k0) * (2 * a.Hkv * HD) + g * HD
+                   : a.part + ((int64_t)part * a.n_tok + kv) * (2 * a.Hkv * HD) + g * HD;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -1034,7 +1149,7 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(AttnBwdArgs a, i
 }
 
 // dK, dV of the parts added up in their order, 4 features per thread
-__global__ __launch_bounds__(256) void attn_dkv_parts_kernel(AttnBwdArgs a, int parts) {
+__global__ __launch_bounds__(256) void attn_dkv_parts_kernel(WinAttnBwdArgs a, int parts) {
   const int kw = a.Hkv * a.hd, w4 = kw / 2;   // 2 kw features of a row, in fours
   const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (idx >= (int64_t)a.n_tok * w4) return;
@@ -1048,7 +1163,28 @@ __global__ __launch_bounds__(256) void attn_dkv_parts_kernel(AttnBwdArgs a, int 
       u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
 
-__global__ __launch_bounds__(256) void attn_delta_bf16_kernel(AttnBwdArgs a) {
+// dK, dV of the far sinks: the sums of their chunks and heads, added up in their order
+__global__ __launch_bounds__(256) void attn_far_sinks_kernel(WinAttnBwdArgs a, int parts) {
+  const int kw = a.Hkv * a.hd, w4 = kw / 2;
+  const int per = (a.n_sink * w4 + 255) / 256;
+  const int start = blockIdx.x / per;   // the segment that starts in this run of kSinkChunk rows
+  const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, start * kSinkChunk + kSinkChunk - 1);
+  const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
+  if (s0 < 0 || s0 / kSinkChunk != start) return;
+  const int idx = blockIdx.x % per * 256 + threadIdx.x, j = idx / w4, col = idx % w4 * 4;
+  if (j >= far_sinks(a, s1 - s0)) return;
+  const int chunks = (s1 - s0 + kSinkChunk - 1) / kSinkChunk;
+  f32x4_t v{0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < chunks; ++c)
+    for (int z = 0; z < parts; ++z)
+      v += *(const f32x4_t *)(a.sink_part +
+                              (((int64_t)(2 * start + c) * parts + z) * far_rows(a) + j) * (2 * kw) + col);
+  if (col < kw) v *= a.scale;
+  *(u32x2_t *)((bf16_t *)a.dqkv + (int64_t)(s0 + j) * (a.Hq + 2 * a.Hkv) * a.hd + a.Hq * a.hd + col) =
+      u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
+}
+
+__global__ __launch_bounds__(256) void attn_delta_bf16_kernel(WinAttnBwdArgs a) {
   const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (idx >= (int64_t)a.n_tok * a.Hq) return;
@@ -1111,15 +1247,19 @@ int attn_row_waves(int n_tok, int n_seg, int heads) {
 // and where one part is taken, 1 / as many as the group has heads:
 //   40 heads, 8 KV: 8000 1298 / 1406; 6 of 4000 2158 / 2445; 28 heads: 40 of
 //   1200 1199 / 1702.
-int attn_dkv_parts(const AttnBwdArgs &a) {
+int attn_dkv_parts(const WinAttnBwdArgs &a) {
   if (!a.part || !aligned16(a.part)) return 1;
   const int group = a.Hq / a.Hkv;
   const int64_t keys = ((int64_t)a.n_tok + 32 * kDkvWaves - 1) / (32 * kDkvWaves) * a.Hkv;
   const int64_t floats = (int64_t)a.n_tok * 2 * a.Hkv * a.hd;   // of a part's sums
-  const double tiles = (double)a.n_tok / a.n_seg / 64 + 1, tile = 1.9 * a.hd / 128;
+  const bool win = windowed(a.window, a.n_tok);
+  const double len = (double)a.n_tok / a.n_seg;
+  // with a window nearly all workgroups see as many queries
+  const double tiles = win ? std::min(len, (double)a.window) / 64 + 2 : len / 64 + 1;
+  const double tile = 1.9 * a.hd / 128;
   auto time = [&](int P) {
     const double top = tile * ((group + P - 1) / P) * tiles + 5, n = (double)keys * P;
-    const double even = (keys * group * tile * (tiles / 2 + 0.5) + n * 5) / 256;
+    const double even = (keys * group * tile * (win ? tiles : tiles / 2 + 0.5) + n * 5) / 256;
     const double t = n <= 256 ? top : std::max(top, even + (a.n_seg == 1 ? 0.1 : 0.6) * top);
     return P == 1 ? t : t + 5 + 8.0 * P * floats / 7e6;
   };
@@ -1130,18 +1270,23 @@ int attn_dkv_parts(const AttnBwdArgs &a) {
   return best;
 }
 
+int attn_dkv_parts(const AttnBwdArgs &a) { return attn_dkv_parts(WinAttnBwdArgs(a)); }
+
 template <int HD>
-static void launch_fwd(const AttnArgs &a, hipStream_t s) {
+static void launch_fwd(const WinAttnArgs &a, hipStream_t s) {
   auto go = [&](auto W) {
     constexpr int NW = decltype(W)::value;
     const int n_qt = (a.n_tok + 32 * NW - 1) / (32 * NW);
-    attn_fwd_mfma_kernel<HD, NW><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
+    if (windowed(a.window, a.n_tok))
+      attn_fwd_mfma_kernel<HD, NW, true><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
+    else
+      attn_fwd_mfma_kernel<HD, NW, false><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
   };
   if (attn_row_waves(a.n_tok, a.n_seg, a.Hq) == 4) go(Ci<4>{});
   else go(Ci<kRowWaves>{});
 }
 
-int attn_fwd_mfma(const AttnArgs &a, hipStream_t s) {
+int attn_fwd_mfma(const WinAttnArgs &a, hipStream_t s) {
   const int tk = timing_begin(s, AJ_KC_ATTN_FWD, 0.0);
   if (a.hd == 128) launch_fwd<128>(a, s);
   else launch_fwd<64>(a, s);
@@ -1149,25 +1294,42 @@ int attn_fwd_mfma(const AttnArgs &a, hipStream_t s) {
   return check_launch("attention forward (mfma)");
 }
 
+size_t attn_sink_floats(int window, int n_sink, int n_tok, int heads, int hd) {
+  if (!windowed(window, n_tok) || n_sink == 0 || n_sink > kFarSinks || n_tok <= std::max(window, kSinkChunk)) return 0;
+  return (size_t)2 * (n_tok / kSinkChunk + 1) * heads * n_sink * 2 * hd;
+}
+
 template <int HD>
-static void launch_bwd(const AttnBwdArgs &a, hipStream_t s) {
+static void launch_bwd(const WinAttnBwdArgs &args, hipStream_t s) {
+  WinAttnBwdArgs a = args;
+  const bool win = windowed(a.window, a.n_tok);
   auto dq = [&](auto W) {
     constexpr int NW = decltype(W)::value;
     const int n_qt = (a.n_tok + 32 * NW - 1) / (32 * NW);
-    attn_dq_mfma_kernel<HD, NW><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
+    if (win) attn_dq_mfma_kernel<HD, NW, true><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
+    else attn_dq_mfma_kernel<HD, NW, false><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
   };
   if (attn_row_waves(a.n_tok, a.n_seg, a.Hq) == 4) dq(Ci<4>{});
   else dq(Ci<kRowWaves>{});
   const int n_kt = (a.n_tok + 32 * kDkvWaves - 1) / (32 * kDkvWaves), parts = attn_dkv_parts(a);
-  attn_dkv_mfma_kernel<HD, kDkvWaves>
-      <<<(unsigned)n_kt * a.Hkv * parts, 64 * kDkvWaves, 0, s>>>(a, parts);
+  const unsigned grid = (unsigned)n_kt * a.Hkv * parts;
+  // the far pass takes one query head of a group per workgroup
+  const int group = a.Hq / a.Hkv, starts = a.n_tok / kSinkChunk + 1;
+  if (!win || attn_sink_floats(a.window, a.n_sink, a.n_tok, a.Hq, HD) == 0) a.sink_part = nullptr;
+  if (win) attn_dkv_mfma_kernel<HD, kDkvWaves, kWindow><<<grid, 64 * kDkvWaves, 0, s>>>(a, parts);
+  else attn_dkv_mfma_kernel<HD, kDkvWaves, kCausal><<<grid, 64 * kDkvWaves, 0, s>>>(a, parts);
+  if (a.sink_part)
+    attn_dkv_mfma_kernel<HD, kDkvWaves, kFar>
+        <<<(unsigned)2 * starts * a.Hq, 64 * kDkvWaves, 0, s>>>(a, group);
   if (parts > 1) {
     const int64_t n4 = (int64_t)a.n_tok * a.Hkv * (a.hd / 2);
     attn_dkv_parts_kernel<<<(unsigned)((n4 + 255) / 256), 256, 0, s>>>(a, parts);
   }
+  if (a.sink_part)   // over the zeros that the window pass left there
+    attn_far_sinks_kernel<<<(unsigned)starts * ((a.n_sink * a.Hkv * (HD / 2) + 255) / 256), 256, 0, s>>>(a, group);
 }
 
-int attn_bwd_mfma(const AttnBwdArgs &a, hipStream_t s) {
+int attn_bwd_mfma(const WinAttnBwdArgs &a, hipStream_t s) {
   const int64_t nd = (int64_t)a.n_tok * a.Hq;
   const int tk = timing_begin(s, AJ_KC_ATTN_BWD, 0.0);
   attn_delta_bf16_kernel<<<(unsigned)((nd + 3) / 4), 256, 0, s>>>(a);

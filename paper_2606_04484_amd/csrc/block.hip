@@ -51,7 +51,7 @@ Saved carve_saved(const aj_block_cfg &c, int n, void *base) {
 
 struct BwdWs {
   void *dy_t, *ds, *dgu, *dx1_t, *dout, *dqkv;
-  float *db, *dx1, *delta, *da, *dg_part, *splitk;
+  float *db, *dx1, *delta, *da, *dg_part, *splitk, *sink;
   size_t splitk_floats;
   size_t bytes;
 };
@@ -79,6 +79,7 @@ BwdWs carve_bwd(const aj_block_cfg &c, int n, void *base) {
   w.splitk_floats = std::max(aj::gemm_partial_floats(2 * F, std::max(d, q), f32),
                              aj::gemm_partial_floats(n, 2 * F, f32));
   w.splitk = cv.take<float>(w.splitk_floats);
+  w.sink = cv.take<float>(f32 ? 0 : aj::attn_sink_floats(c.window, c.n_sink, n, c.n_q_heads, c.head_dim));
   w.bytes = cv.bytes();
   return w;
 }
@@ -250,8 +251,8 @@ int block_fwd(const aj_block_cfg &c, const aj_block_weights &w, const aj_varlen 
   lora_fwd_seg(g, lf, kQkv);
   if ((r = gemm<T>(g, st))) return r;
   rope<T>((T *)sv.qkv, n, v.pos, Hq + Hkv, qdim, hd, c.rope_theta, false, st);
-  AttnArgs at{n, v.n_seg, Hq, Hkv, hd, v.base, v.cu_seqlens, sv.qkv, sv.o, sv.lse,
-              1.0f / sqrtf((float)hd)};
+  WinAttnArgs at(AttnArgs{n, v.n_seg, Hq, Hkv, hd, v.base, v.cu_seqlens, sv.qkv, sv.o, sv.lse,
+                          1.0f / sqrtf((float)hd)});
   at.window = c.window;
   at.n_sink = c.n_sink;
   if ((r = attn_fwd<T>(at, st))) return r;
@@ -352,13 +353,14 @@ int block_bwd(const aj_block_cfg &c, const aj_block_weights &w, const aj_varlen 
   g.B = w.w_o; g.ldb = hq; g.b_kmajor = false; g.C = ws.dout; g.ldc = hq;
   lora_bwd_seg(g, lb, kO, hq);
   if ((r = gemm<T>(g, st))) return r;
-  AttnBwdArgs ab{n, v.n_seg, Hq, Hkv, hd, v.base, v.cu_seqlens, sv.qkv, sv.o, ws.dout, sv.lse,
-                 ws.delta, ws.dqkv, 1.0f / sqrtf((float)hd)};
+  WinAttnBwdArgs ab(AttnBwdArgs{n, v.n_seg, Hq, Hkv, hd, v.base, v.cu_seqlens, sv.qkv, sv.o, ws.dout,
+                                sv.lse, ws.delta, ws.dqkv, 1.0f / sqrtf((float)hd)});
   ab.window = c.window;
   ab.n_sink = c.n_sink;
   if constexpr (sizeof(T) == 2) {   // d gate / d up has been read: scratch
     ab.part = (float *)ws.dgu;
     ab.part_floats = (size_t)n * F;
+    ab.sink_part = ws.sink;
   }
   if ((r = attn_bwd<T>(ab, st))) return r;
   rope<T>((T *)ws.dqkv, n, v.pos, Hq + Hkv, qdim, hd, c.rope_theta, true, st);

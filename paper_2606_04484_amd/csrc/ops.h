@@ -109,12 +109,18 @@ struct AttnArgs {
                         // the matrix-core path, natural log on the plain one unless
                         // lse_log2)
   float scale;
-  int window = 0;       // > 0: a row sees its segment's keys in the last `window` rows
-  int n_sink = 0;       // and the segment's first n_sink ones
-  bool lse_log2 = false;
 };
 template <typename T>
 int attn_fwd(const AttnArgs &a, hipStream_t s);
+// The same with a window
+struct WinAttnArgs : AttnArgs {
+  int window = 0;       // > 0: a row sees its segment's keys in the last `window` rows
+  int n_sink = 0;       // and the segment's first n_sink ones
+  bool lse_log2 = false;
+  explicit WinAttnArgs(const AttnArgs &a) : AttnArgs(a) {}
+};
+template <typename T>
+int attn_fwd(const WinAttnArgs &a, hipStream_t s);
 
 struct AttnBwdArgs {
   int n_tok, n_seg, Hq, Hkv, hd;
@@ -127,22 +133,32 @@ struct AttnBwdArgs {
   float scale;
   float *part = nullptr;    // scratch for dK, dV in parts (16-byte aligned), part_floats of it
   size_t part_floats = 0;
-  int window = 0, n_sink = 0;   // as the forward's
-  bool lse_log2 = false;
 };
 template <typename T>
 int attn_bwd(const AttnBwdArgs &a, hipStream_t s);
+struct WinAttnBwdArgs : AttnBwdArgs {
+  int window = 0, n_sink = 0;   // as the forward's
+  bool lse_log2 = false;
+  float *sink_part = nullptr;   // scratch for the sinks' sums, attn_sink_floats of it
+  explicit WinAttnBwdArgs(const AttnBwdArgs &a) : AttnBwdArgs(a) {}
+};
+template <typename T>
+int attn_bwd(const WinAttnBwdArgs &a, hipStream_t s);
 
 // Whether a window hides anything in a pack of n_tok rows.
 bool windowed(int window, int n_tok);
 
 // bfloat16 MFMA flash attention (head_dim 64 or 128, 16-byte aligned tensors)
 bool attn_mfma_supported(int hd, const void *p0, const void *p1, const void *p2);
-int attn_fwd_mfma(const AttnArgs &a, hipStream_t s);
-int attn_bwd_mfma(const AttnBwdArgs &a, hipStream_t s);
+int attn_fwd_mfma(const WinAttnArgs &a, hipStream_t s);
+int attn_bwd_mfma(const WinAttnBwdArgs &a, hipStream_t s);
+// Floats of scratch that the windowed backward wants for the sums of sinks that see
+// queries past their window (0: none; it grows with n_tok).
+size_t attn_sink_floats(int window, int n_sink, int n_tok, int heads, int hd);
 // its waves per workgroup in the forward and dQ passes, and the parts of a group's
 // query heads in the dK/dV pass
 int attn_row_waves(int n_tok, int n_seg, int heads);
 int attn_dkv_parts(const AttnBwdArgs &a);
+int attn_dkv_parts(const WinAttnBwdArgs &a);
 
 }  // namespace aj
