@@ -594,7 +594,29 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(WinAttnBwdArgs
   // 28 heads of 128: 856 us, 871 spread at each half); four, whose copies take more
   // address registers, would spill then (831 us, 805 spread at each half), except
   // at head_dim 64.
-  const float ndlt = qv ? a.delta[(int64_t)h * a.n_tok + q] : 0.f;
+  float ndlt = 0.f;
+  if constexpr (WIN) {
+    // delta = dO . O here, where dO is in registers already, and kept for the dK/dV
+    // passes: a pass of its own over dO and O took 133 us of 19437 tokens of 28 heads
+    float sum = 0.f;
+    if (qv) {
+      const bf16_t *orow = (const bf16_t *)a.o + (int64_t)q * a.Hq * HD + h * HD + 8 * hl;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const u32x4_t x = *(const u32x4_t *)(orow + 16 * kk);
+        const u32x4_t y = __builtin_bit_cast(u32x4_t, df[kk]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sum = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), sum);
+          sum = fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), sum);
+        }
+      }
+    }
+    ndlt = -(sum + __shfl_xor(sum, 32, 64));
+    if (qv && hl == 0) a.delta[(int64_t)h * a.n_tok + q] = ndlt;
+  } else if (qv) {
+    ndlt = a.delta[(int64_t)h * a.n_tok + q];
+  }
   constexpr bool kSpread = NW >= 8 || HD == 64;
   f32x16_t dp0;
   auto spread = [&](float v) __attribute__((always_inline)) {
@@ -772,23 +794,19 @@ struct DkvSched {
 // its segment's.  Left at that, the workgroup of a long segment's first keys would walk
 // every query of it while the others walk W: where that is a longer way than
 // kSinkChunk, the sinks that see past their window ("far") get no query in the window
-// pass and a pass of their own, cut into chunks of kSinkChunk queries (and, like any dK/dV
-// work, query heads); a last kernel adds the chunks' float32 sums in order.  Chunk c of a
+// pass and a pass of their own (attn_sinks_mfma_kernel), in chunks of kSinkChunk queries
+// of one head; a last kernel adds the chunks' float32 sums in order.  Chunk c of a
 // segment that starts at row s is number 2 floor(s / kSinkChunk) + c: such segments are
 // longer than kSinkChunk, so that their numbers never meet.
 constexpr int kSinkChunk = 1024;
-constexpr int kFarSinks = 128;     // most sinks that the far pass takes (one tile of keys)
+constexpr int kFarSinks = 128;     // most sinks that the far pass takes
 
-// rows of a chunk's sums
-__host__ AJ_DEV int far_rows(const WinAttnBwdArgs &a) { return a.n_sink; }
 AJ_DEV int far_sinks(const WinAttnBwdArgs &a, int seg_len) {
   if (a.sink_part == nullptr || seg_len <= max(a.window, kSinkChunk)) return 0;
   return min(a.n_sink, seg_len - a.window);
 }
 
-enum { kCausal, kWindow, kFar };
-
-template <int HD, int NW, int MODE>
+template <int HD, int NW, bool WIN>
 __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a, int parts) {
   using TT = TokTile<HD, NW>;
   constexpr int KS = HD / 16, DT = HD / 32, T = TT::kBytes, RB = HD * 2;
@@ -810,24 +828,11 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
   const int ld = (a.Hq + 2 * a.Hkv) * HD;
   const int ldo = a.Hq * HD;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, hl = lane >> 5, lq = lane & 31;
-  int k0 = kt * 32 * NW;        // (kFar: kt is the number of a chunk)
-  int qt0 = k0;                 // the first query tile's first row
-  int far_hi = 0, n_far = 0;    // kFar: the chunk's last query, the segment's far sinks
-  if constexpr (MODE == kFar) {
-    const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, kt / 2 * kSinkChunk + kSinkChunk - 1);
-    const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
-    const int chunk = kt - s0 / kSinkChunk * 2;
-    if (s0 < 0 || chunk < 0) return;
-    n_far = far_sinks(a, s1 - s0);
-    if (n_far == 0 || chunk * kSinkChunk >= s1 - s0) return;
-    k0 = s0;
-    qt0 = s0 + chunk * kSinkChunk;
-    far_hi = min(qt0 + kSinkChunk, s1);
-  }
+  const int k0 = kt * 32 * NW;
   const int kv = k0 + 32 * w + lq;            // the key row this lane owns
-  const bool kvv = MODE == kFar ? kv < k0 + n_far : kv < a.n_tok;
-  int ke = kvv ? MODE == kFar ? far_hi : seg_end(a, kv) : 0;    // queries of the key: [kv, ke)
-  if constexpr (MODE == kWindow) {
+  const bool kvv = kv < a.n_tok;
+  int ke = kvv ? seg_end(a, kv) : 0;          // queries of the key: [kv, ke)
+  if constexpr (WIN) {
     if (kvv && ke - kv > a.window) {
       const int s0 = seg_start(a, kv);
       if (kv - s0 >= a.n_sink) ke = kv + a.window;
@@ -836,11 +841,11 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
   }
   const bf16_t *qkv = (const bf16_t *)a.qkv;
   const bf16_t *dout = (const bf16_t *)a.dout;
-  if constexpr (MODE == kWindow) {
+  if constexpr (WIN) {
     const int hi = wave_max(ke);
     if (lane == 0) rng[w] = hi;
   } else if (threadIdx.x == 0) {
-    rng[0] = MODE == kFar ? far_hi : seg_end(a, min(k0 + 32 * NW - 1, a.n_tok - 1));
+    rng[0] = seg_end(a, min(k0 + 32 * NW - 1, a.n_tok - 1));
   }
   bf16x8_t kf[KS], vf[KS];
 #pragma unroll
@@ -873,21 +878,21 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
     }
   }
   __syncthreads();
-  int q_hi = rng[0];          // queries [qt0, q_hi)
-  if constexpr (MODE == kWindow) {
+  int q_hi = rng[0];          // queries [k0, q_hi)
+  if constexpr (WIN) {
 #pragma unroll
     for (int i = 1; i < NW; ++i) q_hi = max(q_hi, rng[i]);
+    q_hi = __builtin_amdgcn_readfirstlane(q_hi);
   }
-  if constexpr (MODE != kCausal) q_hi = __builtin_amdgcn_readfirstlane(q_hi);
   // the part's query heads [h0, h0 + n_h) of the group
   const int group = a.Hq / a.Hkv, h_lo = group * part / parts, n_h = group * (part + 1) / parts - h_lo;
   const int h0 = g * group + h_lo;
-  const int n_qb = q_hi > qt0 ? (q_hi - qt0 + kTR - 1) / kTR : 0;
+  const int n_qb = q_hi > k0 ? (q_hi - k0 + kTR - 1) / kTR : 0;
   const int n_it = n_h * n_qb;
-  // item it: query head h0 + it / n_qb, query tile qt0 + 64 * (it % n_qb)
+  // item it: query head h0 + it / n_qb, query tile k0 + 64 * (it % n_qb)
   auto load_item = [&](int it, auto ST) __attribute__((always_inline)) {
     constexpr int st = decltype(ST)::value;
-    const int h = h0 + it / n_qb, qb = qt0 + kTR * (it % n_qb);
+    const int h = h0 + it / n_qb, qb = k0 + kTR * (it % n_qb);
     TT::load(smq + st * TT::kHalfs, qkv + h * HD, ld, qb, q_hi);
     TT::load(smd + st * TT::kHalfs, dout + h * HD, ldo, qb, q_hi);
     if (w < 2) {                // one float per lane: LSE (wave 0), delta (wave 1)
@@ -1063,8 +1068,8 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
   auto item = [&](const int it, auto ST) __attribute__((always_inline)) {
     constexpr int st = decltype(ST)::value;
     // half tt of item i: row offset o is seen iff o - (lo(i) - 32tt) < span(i)
-    const int lo = kv - (qt0 + kTR * (min(it, n_it - 1) % n_qb)) - 4 * hl;
-    const int lo1 = kv - (qt0 + kTR * (min(it + 1, n_it - 1) % n_qb)) - 4 * hl;
+    const int lo = kv - (k0 + kTR * (min(it, n_it - 1) % n_qb)) - 4 * hl;
+    const int lo1 = kv - (k0 + kTR * (min(it + 1, n_it - 1) % n_qb)) - 4 * hl;
     step(Ci<1>{}, Ci<(st + 2) % 3>{}, Ci<0>{}, Ci<st>{}, Ci<1>{}, Ci<st>{}, Ci<0>{}, lo - 32,
          it < n_it ? span : 0, [] {});
     step(Ci<0>{}, Ci<st>{}, Ci<1>{}, Ci<st>{}, Ci<0>{}, Ci<(st + 1) % 3>{}, Ci<1>{}, lo1,
@@ -1092,7 +1097,7 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
     dma_wait();
     __syncthreads();
     // LSE and delta, then S and dP - delta of half 0
-    const bool whole0 = seen_whole(kv - qt0 - 4 * hl, span);
+    const bool whole0 = seen_whole(kv - k0 - 4 * hl, span);
     read_ld(0, 0);
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
@@ -1104,7 +1109,7 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) asm volatile("" : "+v"(dl[r4]));
       }
-      s = kk == 0 ? s_first(fq, whole0, kv - qt0 - 4 * hl, span) : mfma(fq, kf[kk], s);
+      s = kk == 0 ? s_first(fq, whole0, kv - k0 - 4 * hl, span) : mfma(fq, kf[kk], s);
       dp = mfma(fd, vf[kk], kk == 0 ? delta_init() : dp);
     }
     // the first step's dV/dK group: half -1 (stage 2, cleared)
@@ -1118,10 +1123,8 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
     tail(Ci<2>{});
   }
   if (!kvv) return;
-  if (MODE == kFar || parts > 1) {   // float32 sums of the part's heads, added up by the kernels below
-    float *p = MODE == kFar
-                   ? a.sink_part + (((int64_t)kt * parts + part) * far_rows(a) + kv - k0) * (2 * a.Hkv * HD) + g * HD
-                   : a.part + ((int64_t)part * a.n_tok + kv) * (2 * a.Hkv * HD) + g * HD;
+  if (parts > 1) {   // float32 sums of the part's heads, for attn_dkv_parts_kernel
+    float *p = a.part + ((int64_t)part * a.n_tok + kv) * (2 * a.Hkv * HD) + g * HD;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -1163,24 +1166,163 @@ __global__ __launch_bounds__(256) void attn_dkv_parts_kernel(WinAttnBwdArgs a, i
       u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
 
+// The far sinks' sums over one chunk of queries of one head, 32 keys at a time (a lane
+// owns one).  The keys are few and the queries many, so here the four waves take
+// different queries, blocks of 32 in turn, each staged by its own wave (a ring of two,
+// no barrier), and add up their sums at the end.  What bounds it is the bytes of Q and dO,
+// read once more: in the window pass's kernel (four waves of different keys, one of
+// which has sinks) the same work took 110 us of 19437 tokens of 28 heads of 128.
+template <int HD>
+__global__ __launch_bounds__(256, 1) void attn_sinks_mfma_kernel(WinAttnBwdArgs a, int key_tiles) {
+  constexpr int KS = HD / 16, DT = HD / 32, RB = HD * 2, T = 32 * RB, CPR = HD / 8, RPI = 64 / CPR;
+  constexpr int kCopies = 32 / RPI;
+  // per wave two stages of 32 rows of Q and of dO; at the end its sums
+  __shared__ __attribute__((aligned(16))) char sm[4][4 * T];
+  __shared__ __attribute__((aligned(16))) float stats[4][64];   // a block's LSE and delta
+  static_assert(sizeof(sm[0]) >= 32 * 2 * HD * sizeof(float), "a wave's sums fit its stages");
+  const int group = a.Hq / a.Hkv;
+  const int t = blockIdx.x, h = t % a.Hq, g = h / group;
+  const int key0 = t / a.Hq % key_tiles * 32, slot = t / a.Hq / key_tiles;
+  const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, slot / 2 * kSinkChunk + kSinkChunk - 1);
+  const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
+  const int chunk = slot - s0 / kSinkChunk * 2;
+  if (s0 < 0 || chunk < 0 || chunk * kSinkChunk >= s1 - s0) return;
+  const int n_far = far_sinks(a, s1 - s0);
+  if (key0 >= n_far) return;
+  const int qt0 = s0 + chunk * kSinkChunk, q_hi = min(qt0 + kSinkChunk, s1);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, hl = lane >> 5, lq = lane & 31;
+  const int kv = s0 + key0 + lq;
+  const bool kvv = key0 + lq < n_far;
+  const int ld = (a.Hq + 2 * a.Hkv) * HD, ldo = a.Hq * HD;
+  const bf16_t *qkv = (const bf16_t *)a.qkv, *q_src = qkv + h * HD, *d_src = (const bf16_t *)a.dout + h * HD;
+  TileLanes<HD> L;
+  L.init(sm[w]);
+  bf16x8_t kf[KS], vf[KS];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) {
+    u32x4_t x{0, 0, 0, 0}, y{0, 0, 0, 0};
+    if (kvv) {
+      x = *(const u32x4_t *)(qkv + (int64_t)kv * ld + (a.Hq + g) * HD + 16 * kk + 8 * hl);
+      y = *(const u32x4_t *)(qkv + (int64_t)kv * ld + (a.Hq + a.Hkv + g) * HD + 16 * kk + 8 * hl);
+    }
+    kf[kk] = __builtin_bit_cast(bf16x8_t, x);
+    vf[kk] = __builtin_bit_cast(bf16x8_t, y);
+  }
+  f32x16_t dk[DT], dv[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { dk[i][r] = 0.f; dv[i][r] = 0.f; }
+  const float c = a.scale * kLog2e;
+  const float *ld_src = (hl == 0 ? a.lse : a.delta) + (int64_t)h * a.n_tok;
+  const uint32_t ld_lane = lds_addr(stats[w]) + 16 * hl;
+  const int n_blk = (q_hi - qt0 + 31) / 32;
+  float next = 0.f;
+  auto load = [&](const int b, const int st) __attribute__((always_inline)) {
+    const int r0 = qt0 + 32 * b;
+    uint16_t *dst = (uint16_t *)(sm[w] + st * 2 * T);
+#pragma unroll
+    for (int q = 0; q < kCopies; ++q) {
+      const int r = q * RPI + lane / CPR, ch = (lane % CPR) ^ tok_swz<HD>(r);
+      const int64_t rr = min(r0 + r, q_hi - 1);
+      __builtin_amdgcn_global_load_lds(q_src + rr * ld + 8 * ch,
+                                       (__attribute__((address_space(3))) void *)(dst + q * 512), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(d_src + rr * ldo + 8 * ch,
+                                       (__attribute__((address_space(3))) void *)(dst + T / 2 + q * 512), 16,
+                                       0, 0);
+    }
+    next = ld_src[min(r0 + lq, q_hi - 1)];
+  };
+  auto block = [&](const int b, const int st) __attribute__((always_inline)) {
+    const int q0 = qt0 + 32 * b;
+    dma_wait();        // the block's rows and its LSE and delta
+    stats[w][lane] = next;
+    asm volatile("" ::: "memory");
+    if (b + 4 < n_blk) load(b + 4, st ^ 1);
+    f32x4_t lv[4], dl[4];
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      lv[r4] = lds_read_f4(ld_lane, 8 * r4 * 4);
+      dl[r4] = lds_read_f4(ld_lane, 128 + 8 * r4 * 4);
+    }
+    lds_wait();
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) asm volatile("" : "+v"(lv[r4]), "+v"(dl[r4]));
+    f32x16_t s, dp, dp0;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp0[r] = dl[r >> 2][r & 3];
+    rows_times_pair<HD>(s, dp, L, st * 2 * T, st * 2 * T + T, 0, kf, vf, dp0);
+    // seen by every key of the tile, and none of the rows behind the chunk
+    const bool whole = q0 >= s0 + key0 + 31 && q0 + 32 <= q_hi;
+    f32x16_t p;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int q = q0 + 4 * hl + 8 * (r >> 2) + (r & 3);
+      const float e = fast_exp2(fmaf(s[r], c, -lv[r >> 2][r & 3]));
+      p[r] = whole | ((q >= kv) & (q < q_hi)) ? e : 0.f;
+      s[r] = p[r] * dp[r];
+    }
+    const bf16x8_t pj[2] = {pack8(p, 0), pack8(p, 8)}, sj[2] = {pack8(s, 0), pack8(s, 8)};
+    cols_times_half<HD>(dv, L, st * 2 * T + T, 0, pj);   // dV^T += dO^T P
+    cols_times_half<HD>(dk, L, st * 2 * T, 0, sj);       // dK^T += Q^T dS
+  };
+  if (w < n_blk) load(w, 0);
+  for (int b = w; b < n_blk; b += 8) {
+    block(b, 0);
+    if (b + 4 < n_blk) block(b + 4, 1);
+  }
+  __syncthreads();
+  float *mine = (float *)sm[w] + lq * 2 * HD;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int d = 32 * i + 8 * r4 + 4 * hl;
+      *(f32x4_t *)(mine + d) = f32x4_t{dk[i][4 * r4], dk[i][4 * r4 + 1], dk[i][4 * r4 + 2], dk[i][4 * r4 + 3]};
+      *(f32x4_t *)(mine + HD + d) =
+          f32x4_t{dv[i][4 * r4], dv[i][4 * r4 + 1], dv[i][4 * r4 + 2], dv[i][4 * r4 + 3]};
+    }
+  __syncthreads();
+  for (int e = threadIdx.x * 4; e < min(32, n_far - key0) * 2 * HD; e += 1024) {
+    f32x4_t v = *(const f32x4_t *)((const float *)sm[0] + e);
+#pragma unroll
+    for (int x = 1; x < 4; ++x) v += *(const f32x4_t *)((const float *)sm[x] + e);
+    const int key = key0 + e / (2 * HD), d = e % (2 * HD);
+    *(f32x4_t *)(a.sink_part + (((int64_t)slot * a.Hq + h) * a.n_sink + key) * (2 * HD) + d) = v;
+  }
+}
+
 // dK, dV of the far sinks: the sums of their chunks and heads, added up in their order
-__global__ __launch_bounds__(256) void attn_far_sinks_kernel(WinAttnBwdArgs a, int parts) {
-  const int kw = a.Hkv * a.hd, w4 = kw / 2;
-  const int per = (a.n_sink * w4 + 255) / 256;
+// (64 columns of four features a workgroup, a quarter of the sums per wave).
+__global__ __launch_bounds__(256) void attn_far_sinks_kernel(WinAttnBwdArgs a) {
+  const int group = a.Hq / a.Hkv, w4 = a.hd / 2;   // 2 hd features of a key and KV head, in fours
+  const int per = (a.n_sink * a.Hkv * w4 + 63) / 64;
   const int start = blockIdx.x / per;   // the segment that starts in this run of kSinkChunk rows
   const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, start * kSinkChunk + kSinkChunk - 1);
   const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
   if (s0 < 0 || s0 / kSinkChunk != start) return;
-  const int idx = blockIdx.x % per * 256 + threadIdx.x, j = idx / w4, col = idx % w4 * 4;
-  if (j >= far_sinks(a, s1 - s0)) return;
-  const int chunks = (s1 - s0 + kSinkChunk - 1) / kSinkChunk;
+  const int n_far = far_sinks(a, s1 - s0);
+  if (n_far == 0) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int idx = blockIdx.x % per * 64 + lane;
+  const int col = idx % w4 * 4, g = idx / w4 % a.Hkv, j = idx / w4 / a.Hkv;
+  const int n = (s1 - s0 + kSinkChunk - 1) / kSinkChunk * group;   // (chunk, head of the group)
+  __shared__ f32x4_t red[4][64];
   f32x4_t v{0.f, 0.f, 0.f, 0.f};
-  for (int c = 0; c < chunks; ++c)
-    for (int z = 0; z < parts; ++z)
-      v += *(const f32x4_t *)(a.sink_part +
-                              (((int64_t)(2 * start + c) * parts + z) * far_rows(a) + j) * (2 * kw) + col);
-  if (col < kw) v *= a.scale;
-  *(u32x2_t *)((bf16_t *)a.dqkv + (int64_t)(s0 + j) * (a.Hq + 2 * a.Hkv) * a.hd + a.Hq * a.hd + col) =
+  if (j < n_far) {
+    const float *p = a.sink_part + ((int64_t)2 * start * a.Hq * a.n_sink + j) * (2 * a.hd) + col;
+#pragma unroll 8
+    for (int i = w; i < n; i += 4)
+      v += *(const f32x4_t *)(p + ((int64_t)(i / group) * a.Hq + g * group + i % group) * a.n_sink * (2 * a.hd));
+  }
+  red[w][lane] = v;
+  __syncthreads();
+  if (w > 0 || j >= n_far) return;
+  v = red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane];
+  const bool is_k = col < a.hd;
+  if (is_k) v *= a.scale;
+  *(u32x2_t *)((bf16_t *)a.dqkv + (int64_t)(s0 + j) * (a.Hq + 2 * a.Hkv) * a.hd +
+               (a.Hq + (is_k ? g : a.Hkv + g)) * a.hd + (is_k ? col : col - a.hd)) =
       u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
 
@@ -1272,17 +1414,26 @@ int attn_dkv_parts(const WinAttnBwdArgs &a) {
 
 int attn_dkv_parts(const AttnBwdArgs &a) { return attn_dkv_parts(WinAttnBwdArgs(a)); }
 
+// With a window four waves, whose workgroup reads window + 128 keys where eight read
+// window + 256.  Forward / dQ, 4 waves against 8, us: 19437 tokens of 28 heads, window 128
+// 167 / 209 against 223 / 283; 1024 393 / 482 against 404 / 514; 20000 of them, 4096 996 /
+// 1316 against 1015 / 1320; 32771 of 40 heads, 2048 1527 / 1976 against 1550 / 2000; 14511 of
+// 28 heads of 64, 1024 147 / 201 against 202 / 233.
+template <typename A> static int window_waves(const A &a) {
+  return windowed(a.window, a.n_tok) ? 4 : attn_row_waves(a.n_tok, a.n_seg, a.Hq);
+}
+
 template <int HD>
 static void launch_fwd(const WinAttnArgs &a, hipStream_t s) {
   auto go = [&](auto W) {
     constexpr int NW = decltype(W)::value;
     const int n_qt = (a.n_tok + 32 * NW - 1) / (32 * NW);
-    if (windowed(a.window, a.n_tok))
-      attn_fwd_mfma_kernel<HD, NW, true><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
+    if (NW == 4 && windowed(a.window, a.n_tok))
+      attn_fwd_mfma_kernel<HD, 4, true><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
     else
       attn_fwd_mfma_kernel<HD, NW, false><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
   };
-  if (attn_row_waves(a.n_tok, a.n_seg, a.Hq) == 4) go(Ci<4>{});
+  if (window_waves(a) == 4) go(Ci<4>{});
   else go(Ci<kRowWaves>{});
 }
 
@@ -1306,33 +1457,33 @@ static void launch_bwd(const WinAttnBwdArgs &args, hipStream_t s) {
   auto dq = [&](auto W) {
     constexpr int NW = decltype(W)::value;
     const int n_qt = (a.n_tok + 32 * NW - 1) / (32 * NW);
-    if (win) attn_dq_mfma_kernel<HD, NW, true><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
+    if (NW == 4 && win) attn_dq_mfma_kernel<HD, 4, true><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
     else attn_dq_mfma_kernel<HD, NW, false><<<(unsigned)n_qt * a.Hq, 64 * NW, 0, s>>>(a, n_qt);
   };
-  if (attn_row_waves(a.n_tok, a.n_seg, a.Hq) == 4) dq(Ci<4>{});
+  if (window_waves(a) == 4) dq(Ci<4>{});
   else dq(Ci<kRowWaves>{});
   const int n_kt = (a.n_tok + 32 * kDkvWaves - 1) / (32 * kDkvWaves), parts = attn_dkv_parts(a);
   const unsigned grid = (unsigned)n_kt * a.Hkv * parts;
-  // the far pass takes one query head of a group per workgroup
-  const int group = a.Hq / a.Hkv, starts = a.n_tok / kSinkChunk + 1;
+  const int starts = a.n_tok / kSinkChunk + 1;
   if (!win || attn_sink_floats(a.window, a.n_sink, a.n_tok, a.Hq, HD) == 0) a.sink_part = nullptr;
-  if (win) attn_dkv_mfma_kernel<HD, kDkvWaves, kWindow><<<grid, 64 * kDkvWaves, 0, s>>>(a, parts);
-  else attn_dkv_mfma_kernel<HD, kDkvWaves, kCausal><<<grid, 64 * kDkvWaves, 0, s>>>(a, parts);
+  if (win) attn_dkv_mfma_kernel<HD, kDkvWaves, true><<<grid, 64 * kDkvWaves, 0, s>>>(a, parts);
+  else attn_dkv_mfma_kernel<HD, kDkvWaves, false><<<grid, 64 * kDkvWaves, 0, s>>>(a, parts);
+  const int key_tiles = (a.n_sink + 31) / 32;
   if (a.sink_part)
-    attn_dkv_mfma_kernel<HD, kDkvWaves, kFar>
-        <<<(unsigned)2 * starts * a.Hq, 64 * kDkvWaves, 0, s>>>(a, group);
+    attn_sinks_mfma_kernel<HD><<<(unsigned)2 * starts * key_tiles * a.Hq, 256, 0, s>>>(a, key_tiles);
   if (parts > 1) {
     const int64_t n4 = (int64_t)a.n_tok * a.Hkv * (a.hd / 2);
     attn_dkv_parts_kernel<<<(unsigned)((n4 + 255) / 256), 256, 0, s>>>(a, parts);
   }
   if (a.sink_part)   // over the zeros that the window pass left there
-    attn_far_sinks_kernel<<<(unsigned)starts * ((a.n_sink * a.Hkv * (HD / 2) + 255) / 256), 256, 0, s>>>(a, group);
+    attn_far_sinks_kernel<<<(unsigned)starts * ((a.n_sink * a.Hkv * (HD / 2) + 63) / 64), 256, 0, s>>>(a);
 }
 
 int attn_bwd_mfma(const WinAttnBwdArgs &a, hipStream_t s) {
   const int64_t nd = (int64_t)a.n_tok * a.Hq;
   const int tk = timing_begin(s, AJ_KC_ATTN_BWD, 0.0);
-  attn_delta_bf16_kernel<<<(unsigned)((nd + 3) / 4), 256, 0, s>>>(a);
+  if (!windowed(a.window, a.n_tok))   // (the windowed dQ pass forms delta itself)
+    attn_delta_bf16_kernel<<<(unsigned)((nd + 3) / 4), 256, 0, s>>>(a);
   if (a.hd == 128) launch_bwd<128>(a, s);
   else launch_bwd<64>(a, s);
   timing_end(s, tk);
