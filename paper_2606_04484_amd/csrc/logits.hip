@@ -31,6 +31,15 @@ template <typename V> AJ_DEV V wave_sum(V v) {
   return v;
 }
 
+// LDS writes (or reads) complete, then a barrier.  __syncthreads would wait for the loads
+// of the next values too, which are to be on their way meanwhile (top k of 4096 rows of 152064
+// float32: 702 us with it).
+AJ_DEV void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // A row's values by u = v + shift; runs start at multiples of kRun.
 template <typename T>
 struct Row {
@@ -62,6 +71,31 @@ struct Row {
     }
     return b;
   }
+  // the run at u if it lies in the row as a whole, else all -inf: what that leaves out
+  // are the values before the row's first and behind its last boundary, `rim` by number
+  AJ_DEV Bits whole(int u) const {
+    Bits b;
+    if (u >= shift && u + kRun<T> <= end) b.w = *reinterpret_cast<const uint4 *>(aligned + (uint32_t)u);
+    else b.w.x = b.w.y = b.w.z = b.w.w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    return b;
+  }
+  // u of rim value i in [0, 2 kRun), or -1
+  AJ_DEV int rim(int i) const {
+    const int last = max(end & -kRun<T>, shift > 0 ? kRun<T> : 0);   // (one run may hold both ends)
+    const int u = i < kRun<T> ? i : last + i - kRun<T>;
+    return (i < kRun<T> ? shift > 0 && u >= shift : i < 2 * kRun<T>) && u < end ? u : -1;
+  }
+  // N runs of a thread, `stride` values apart from u + at on; [u, u + span) holds all threads'
+  template <int N> AJ_DEV void load(Bits (&b)[N], int u, int at, int stride, int span) const {
+    if (u >= shift && u + span <= end) {
+      const T *p = aligned + u;
+#pragma unroll
+      for (int q = 0; q < N; ++q) b[q].w = *reinterpret_cast<const uint4 *>(p + (uint32_t)(q * stride + at));
+    } else {
+#pragma unroll
+      for (int q = 0; q < N; ++q) b[q] = load(u + q * stride + at);
+    }
+  }
   AJ_DEV static void values(const Bits &b, float (&z)[kRun<T>]) {
     const uint32_t w[4] = {b.w.x, b.w.y, b.w.z, b.w.w};
     if constexpr (sizeof(T) == 4) {
@@ -79,239 +113,363 @@ struct Row {
 
 // ------------------------------------------------------------------ top k
 // Order of values: larger first, equal ones (-0 and 0 among them) by the lower index, NaN
-// before all.  A value's place is one 64-bit number, its order-keeping bits above the
+// before all.  A value's place is one number, its order-keeping bits above the
 // complement of its index, so that no two are equal.
+constexpr uint32_t kNaNOrder = 0xff800001u;      // +inf's and one
+constexpr int kIndexBits = 24;                      // vocab <= 2^24
+constexpr uint64_t kAbove = (uint64_t)(kNaNOrder + 1) << kIndexBits;     // above every place
 AJ_DEV uint32_t order_bits(float z) {
   const uint32_t u = __float_as_uint(z + 0.f);
-  return z != z ? 0xffffffffu : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return z != z ? kNaNOrder : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-AJ_DEV uint64_t place(float z, int v) { return (uint64_t)order_bits(z) << 32 | (uint32_t)~v; }
+AJ_DEV uint64_t place(float z, int v) {
+  return (uint64_t)order_bits(z) << kIndexBits | (~(uint32_t)v & ((1u << kIndexBits) - 1));
+}
+AJ_DEV int place_index(uint64_t p) { return (int)(~(uint32_t)p & ((1u << kIndexBits) - 1)); }
+// the value of such bits (-inf for bits below its own)
 AJ_DEV float order_value(uint32_t o) {
-  return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+  return o <= 0x007fffffu ? -INFINITY : __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-constexpr int kTopNT = 512, kTopWaves = kTopNT / 64;
-constexpr int kTopCap = 2048;    // candidates kept in LDS
+constexpr int kTopNT = 256, kTopWaves = kTopNT / 64;
+constexpr int kTopCap = 1024;    // candidates kept in LDS
+constexpr int kSlack = 64;       // over k that a last cut may leave to the ranking
 
-// The sum of v over the workgroup, in every thread.
-AJ_DEV int block_sum(int v, int *red) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  int s = 0;
-  for (int w = 0; w < (int)blockDim.x / 64; ++w) s += red[w];
-  return s;
-}
-
-// The kk-th largest of the places that `count(t)`, the number at or above t in this
-// thread, tells of.
+// A threshold in [lo, hi) that kk places reach and no more than `most`, where kk and more
+// reach lo and fewer hi; `count(t)` tells how many of its wave do.  (A bisection: places
+// are spread, so where `most` leaves some room a dozen steps find one; that equal values
+// are told apart by their indices alone takes 24 more.)
 template <typename F>
-AJ_DEV uint64_t kth_place(int kk, int *red, F count) {
-  uint64_t t = 0;
-  for (int b = 63; b >= 0; --b) {
-    const uint64_t c = t | (uint64_t)1 << b;
-    if (block_sum(count(c), red) >= kk) t = c;
+AJ_DEV uint64_t kth_place(int kk, int most, uint64_t lo, uint64_t hi, int (*red)[kTopWaves], F count) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int slot = 0;      // (three in turn: one barrier a step)
+  lds_barrier();
+  for (uint64_t t = lo;; t = lo + (hi - lo) / 2) {
+    const int mine = count(t);
+    if (lane == 0) red[slot][wave] = mine;
+    lds_barrier();
+    const int n = __builtin_amdgcn_readfirstlane(red[slot][0] + red[slot][1] + red[slot][2] + red[slot][3]);
+    slot = slot == 2 ? 0 : slot + 1;
+    if (n >= kk) lo = t;
+    else hi = t;
+    if ((n >= kk && n <= most) || hi - lo <= 1) break;
   }
+  return lo;
+}
+
+// The kk largest of the n places of `in`, of which all reach lo, and some next ones, `most`
+// in all, to `out` (in no order); the return value is a threshold that these reach and
+// no other.
+constexpr int kHold = kTopCap / kTopNT;
+AJ_DEV uint64_t cut(const uint64_t *in, int n, int kk, int most, uint64_t lo, uint64_t *out, int (*red)[kTopWaves],
+                    int *n_out) {
+  uint64_t v[kHold], largest = 0;
+#pragma unroll
+  for (int h = 0; h < kHold; ++h) {
+    const int i = h * kTopNT + threadIdx.x;
+    v[h] = i < n ? in[i] : 0;
+    largest = max(largest, v[h]);
+  }
+  const uint32_t top = wave_max((uint32_t)(largest >> kIndexBits));
+  lds_barrier();
+  if (threadIdx.x == 0) *n_out = 0;
+  if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = (int)top;
+  lds_barrier();
+  uint32_t hi = 0;
+#pragma unroll
+  for (int w = 0; w < kTopWaves; ++w) hi = max(hi, (uint32_t)red[0][w]);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  const uint64_t t = kth_place(kk, most, max(lo, (uint64_t)1), (uint64_t)(hi + 1) << kIndexBits, red, [&](uint64_t p) {
+    int c = 0;
+#pragma unroll
+    for (int h = 0; h < kHold; ++h) c += __popcll(__builtin_amdgcn_ballot_w64(v[h] >= p));
+    return c;
+  });
+#pragma unroll
+  for (int h = 0; h < kHold; ++h)
+    if (v[h] >= t) out[atomicAdd(n_out, 1)] = v[h];
+  lds_barrier();
   return t;
 }
 
-// Largest to smallest: out[r] = the place with r larger ones among the n of c (LDS), r < kk
-AJ_DEV void write_ranked(const uint64_t *c, int n, int kk, uint64_t *out) {
+// Largest to smallest: out[r] = the place with r larger ones among the n of c (LDS, room
+// for kRankPad more), r < kk.  Every thread counts for a candidate of its own, 16 of the
+// others at a time: as many LDS reads in flight cover each other's latency (one at a time
+// took 5 us of 200 candidates).  The time goes with n^2, so longer lists are cut first.
+constexpr int kRankPad = 16;
+AJ_DEV void write_ranked(uint64_t *c, int n, int kk, uint64_t *out) {
+  if (threadIdx.x < kRankPad) c[n + threadIdx.x] = 0;
+  lds_barrier();
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const uint64_t mine = c[i];
     int r = 0;
-    for (int j = 0; j < n; ++j) r += c[j] > mine;
+    for (int j = 0; j < n; j += kRankPad) {
+      ulonglong2 v[kRankPad / 2];
+#pragma unroll
+      for (int q = 0; q < kRankPad / 2; ++q) v[q] = *reinterpret_cast<const ulonglong2 *>(c + j + 2 * q);
+#pragma unroll
+      for (int q = 0; q < kRankPad / 2; ++q) r += (int)(v[q].x > mine) + (int)(v[q].y > mine);
+    }
     if (r < kk) out[r] = mine;
   }
 }
 
-// One workgroup per part of a row: kTopNT * E values held in registers.  Gives
-// the part's k largest places in order (0 after the last), its maximum and its sum of
-// exp2((z - max) c).
+// One workgroup per part [u0, u0 + width) of a row, kTopNT * E values at a time, the next
+// ones on their way meanwhile.  Gives the part's k largest places in order (0 after the
+// last), and its sum of 2^(z c) as a power of two (log2 units) and a factor.
 //
-// A threshold that at least k values reach comes from the threads' maxima: in every
-// wave the ceil(k / 8)-th largest of its 64 (a bisection over the bits with one ballot
-// a step, to 20 bits: a lower threshold is as right), and of these the smallest.  The
-// values at or above it, about k of them, are ranked by counting.  Where equal values
-// or a NaN break that, a bisection over the places finds the k-th itself.
+// Values not below a threshold that k of those met so far reach go to a list in LDS.
+// The first threshold comes from the threads' maxima (two each): in every wave the
+// ceil(k / 4)-th largest of its 128 (a bisection over the bits with ballots, to 20 bits:
+// a lower threshold is as right), and of these the smallest.  Later ones are the k-th
+// of the list (or one a little lower), which is cut whenever twice k and more are in it, so
+// that of a long row few values pass.  Where too many pass all the same (equal values, NaN,
+// which is never below), a bisection over the places finds the k-th itself.
 template <typename T, int E>
-__global__ __launch_bounds__(kTopNT) void topk_part_kernel(const void *logits, int64_t ld, int vocab,
-                                                           int parts, int k, float c,
-                                                           uint64_t *cand, float2 *ms) {
-  constexpr int R = kRun<T>, Q = E / R;
-  __shared__ uint64_t list[kTopCap];
+__global__ __launch_bounds__(kTopNT, E == 32 ? 4 : 5) void topk_part_kernel(
+    const void *logits, int64_t ld, int vocab, int parts, int width, int k, float c, uint64_t *cand,
+    float2 *ms) {
+  constexpr int R = kRun<T>, Q = E / R, C = kTopNT * E;
+  __shared__ __attribute__((aligned(16))) uint64_t list[2][kTopCap + kRankPad];
   __shared__ float red_m[kTopWaves], red_s[kTopWaves];
   __shared__ uint32_t red_t[kTopWaves];
-  __shared__ int red_i[kTopWaves], n_list;
+  __shared__ int red_i[3][kTopWaves], added[3], n_kept;
   const int64_t row = blockIdx.x / parts;
   const int part = blockIdx.x % parts;
   const Row<T> x(logits, row, ld, vocab);
-  const int u0 = part * kTopNT * E + threadIdx.x * R;
+  const int u0 = part * width, u1 = min(u0 + width, x.end);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   typename Row<T>::Bits b[Q];
+  auto fetch = [&](int u) __attribute__((always_inline)) {
+    if (u >= x.shift && u + C <= x.end) {
+      const T *p = x.aligned + u;
 #pragma unroll
-  for (int q = 0; q < Q; ++q) b[q] = x.load(u0 + q * kTopNT * R);
-  float z[E];
+      for (int q = 0; q < Q; ++q) b[q].w = *reinterpret_cast<const uint4 *>(p + (q * kTopNT + threadIdx.x) * R);
+    } else {
 #pragma unroll
-  for (int q = 0; q < Q; ++q) {
-    float t[R];
-    Row<T>::values(b[q], t);
+      for (int q = 0; q < Q; ++q) b[q] = x.whole(u + (q * kTopNT + threadIdx.x) * R);
+    }
+  };
+  fetch(u0);
+  // the row's rim goes with its first part, a value for each of some threads
+  const int rim = part == 0 && threadIdx.x < 2 * R ? x.rim(threadIdx.x) : -1;
+  const float zr = rim >= 0 ? ldf(x.aligned + rim) : -INFINITY;
+  if (threadIdx.x < 3) added[threadIdx.x] = 0;
+  int cur = 0, have = 0;      // the list in use and what it holds
+  uint64_t least = 0;         // the least place that goes to it
+  float tau = -INFINITY;      // ... and its value
+  float ref = -INFINITY, s = 0.f;
+  int turn = 0;
+  for (int u = u0; u < u1; u += C) {
+    float z[E];
 #pragma unroll
-    for (int j = 0; j < R; ++j) z[q * R + j] = t[j];
+    for (int q = 0; q < Q; ++q) {
+      float t[R];
+      Row<T>::values(b[q], t);
+#pragma unroll
+      for (int j = 0; j < R; ++j) z[q * R + j] = t[j];
+    }
+    if (u + C < u1) fetch(u + C);
+    const bool first = u == u0;
+    float top[Q], m0 = first ? zr : -INFINITY, m1 = -INFINITY;       // top: of each run
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      top[q] = z[q * R];
+#pragma unroll
+      for (int j = 1; j < R; ++j) top[q] = fmaxf(top[q], z[q * R + j]);
+      if (q & 1) m1 = fmaxf(m1, top[q]);
+      else m0 = fmaxf(m0, top[q]);
+    }
+    // s counts in units of 2^ref, ref the rounded product of the largest value and c
+    const float n = fmaxf(ref, fmaxf(m0, m1) * c), base = n == -INFINITY ? 0.f : n;
+    s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
+    ref = n;
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += fast_exp2(fmaf(z[e], c, -base));
+    if (first) {
+      s += fast_exp2(fmaf(zr, c, -base));
+      const uint32_t o0 = order_bits(m0), o1 = order_bits(m1);
+      const int j = (k + kTopWaves - 1) / kTopWaves;
+      uint32_t t = 0;
+      for (int bit = 31; bit >= 12; --bit) {
+        const uint32_t v = t | 1u << bit;
+        if (__popcll(__builtin_amdgcn_ballot_w64(o0 >= v)) + __popcll(__builtin_amdgcn_ballot_w64(o1 >= v)) >= j)
+          t = v;
+      }
+      if (lane == 0) red_t[wave] = t;
+      lds_barrier();
+      t = min(min(red_t[0], red_t[1]), min(red_t[2], red_t[3]));
+      t = __builtin_amdgcn_readfirstlane(t);
+      tau = order_value(t);
+      least = (uint64_t)t << kIndexBits;
+    }
+    // the place of value e, 0 outside the row
+    const int at0 = u + (int)threadIdx.x * R - x.shift;
+    auto place_of = [&](int e) {
+      // through copies that the compiler does not see into, or it forms every place ahead
+      // of the loops that want them, for which there are no registers
+      float ze = z[e];
+      int a = at0;
+      asm volatile("" : "+v"(ze), "+v"(a));
+      const int v = a + (e / R) * kTopNT * R + e % R;
+      const int ur = v - e % R + x.shift;      // its run; the rim is not among them
+      return ur >= x.shift && ur + R <= x.end ? place(ze, v) : 0;
+    };
+    auto add = [&](uint64_t p) {
+      if (p < least || p == 0) return;
+      const int at = have + atomicAdd(&added[turn], 1);
+      if (at < kTopCap) list[cur][at] = p;
+    };
+    // a thread whose sum is NaN has met a NaN (which no maximum shows) or +inf: it
+    // looks at all it holds
+    float bar = s == s ? tau : -INFINITY;
+    for (;;) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+        if (__builtin_amdgcn_ballot_w64(!(top[q] < bar))) {
+#pragma unroll
+          for (int j = 0; j < R; ++j) add(place_of(q * R + j));
+        }
+      if (first && rim >= 0) add(place(zr, rim - x.shift));
+      // (the next turn's counter was last read two turns ago)
+      const int now = turn;
+      turn = turn == 2 ? 0 : turn + 1;
+      if (threadIdx.x == 0) added[turn] = 0;
+      lds_barrier();
+      const int n_list = have + added[now];
+      if (n_list <= kTopCap) {
+        have = n_list;
+        break;
+      }
+      // too many: again with the k-th place of the list as it was and these values
+      auto count = [&](uint64_t p) {
+        int cnt = 0;
+        for (int i = 0; i < have; i += kTopNT)
+          cnt += __popcll(__builtin_amdgcn_ballot_w64(i + (int)threadIdx.x < have &&
+                                                      list[cur][i + threadIdx.x] >= p));
+#pragma unroll
+        for (int e = 0; e < E; ++e) cnt += __popcll(__builtin_amdgcn_ballot_w64(place_of(e) >= p));
+        if (first)
+          cnt += __popcll(__builtin_amdgcn_ballot_w64(rim >= 0 && place(zr, rim - x.shift) >= p));
+        return cnt;
+      };
+      least = kth_place(k, k, 1, kAbove, red_i, count);
+      bar = -INFINITY;
+      if (threadIdx.x == 0) n_kept = 0;
+      lds_barrier();
+      for (int i = threadIdx.x; i < have; i += kTopNT)
+        if (list[cur][i] >= least) list[cur ^ 1][atomicAdd(&n_kept, 1)] = list[cur][i];
+      lds_barrier();
+      have = __builtin_amdgcn_readfirstlane(n_kept);
+      cur ^= 1;
+      tau = order_value((uint32_t)(least >> kIndexBits));
+    }
+    if (have >= 2 * k + 64 && u + C < u1) {
+      least = cut(list[cur], have, k, k + k / 4 + 32, least, list[cur ^ 1], red_i, &n_kept);
+      cur ^= 1;
+      have = __builtin_amdgcn_readfirstlane(n_kept);
+      tau = order_value((uint32_t)(least >> kIndexBits));
+    }
   }
-  auto index = [&](int e) { return u0 + (e / R) * kTopNT * R + e % R - x.shift; };
-  auto inside = [&](int e) { return (unsigned)index(e) < (unsigned)vocab; };
-  float m = -INFINITY;
-#pragma unroll
-  for (int e = 0; e < E; ++e) m = fmaxf(m, z[e]);
-  // the wave's threshold
-  const uint32_t mo = order_bits(m);
-  const int j = (k + kTopWaves - 1) / kTopWaves;
-  uint32_t t = 0;
-  for (int bit = 31; bit >= 12; --bit) {
-    const uint32_t try_t = t | 1u << bit;
-    if (__popcll(__builtin_amdgcn_ballot_w64(mo >= try_t)) >= j) t = try_t;
+  if (have > k + 128) {
+    cut(list[cur], have, k, k + kSlack, least, list[cur ^ 1], red_i, &n_kept);
+    cur ^= 1;
+    have = __builtin_amdgcn_readfirstlane(n_kept);
   }
-  const float wm = wave_max(m);
-  if (threadIdx.x == 0) n_list = 0;
-  if (lane == 0) {
-    red_m[wave] = wm;
-    red_t[wave] = t;
-  }
+  const float wm = wave_max(ref);
+  if (lane == 0) red_m[wave] = wm;
   __syncthreads();
-  float M = red_m[0];
-  t = red_t[0];
-#pragma unroll
-  for (int w = 1; w < kTopWaves; ++w) {
-    M = fmaxf(M, red_m[w]);
-    t = min(t, red_t[w]);
-  }
-  // the partial log-sum-exp, and the candidates
-  const float base = M == -INFINITY ? 0.f : M;
-  float s = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) s += fast_exp2((z[e] - base) * c);
-  const float tau = t <= order_bits(-INFINITY) ? -INFINITY : order_value(t);
-  int mine = 0;
-#pragma unroll
-  for (int e = 0; e < E; ++e) mine += inside(e) & (z[e] >= tau);
-  int at = mine;      // inclusive prefix over the wave, then the wave's place in the list
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(at, o, 64);
-    if (lane >= o) at += v;
-  }
-  int first = 0;
-  if (lane == 63) first = atomicAdd(&n_list, at);
-  at += __shfl(first, 63, 64) - mine;
-  s = wave_sum(s);
+  const float M = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+  s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - M));
   if (lane == 0) red_s[wave] = s;
-  __syncthreads();
-  float S = 0.f;
-#pragma unroll
-  for (int w = 0; w < kTopWaves; ++w) S += red_s[w];
-  if (threadIdx.x == 0) ms[blockIdx.x] = make_float2(M, S);
   uint64_t *out = cand + (int64_t)blockIdx.x * k;
-  const int lo = part * kTopNT * E, kk =
-      max(0, min(k, min(x.end, lo + kTopNT * E) - max(x.shift, lo)));
-  int n = n_list;
-  uint64_t least = 0;
-  // S is NaN where a NaN (or +inf, whose own difference is one) is among the values
-  const bool listed = n >= kk && n <= kTopCap && S == S;
-  if (!listed) {
-    least = kth_place(kk, red_i, [&](uint64_t p) {
-      int cnt = 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) cnt += inside(e) & (place(z[e], index(e)) >= p);
-      return cnt;
-    });
-    __syncthreads();
-    if (threadIdx.x == 0) n_list = 0;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (inside(e) & (place(z[e], index(e)) >= least)) list[atomicAdd(&n_list, 1)] = place(z[e], index(e));
-    n = kk;
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (inside(e) & (z[e] >= tau)) list[at++] = place(z[e], index(e));
-  }
-  __syncthreads();
-  write_ranked(list, n, kk, out);
-  for (int i = kk + threadIdx.x; i < k; i += kTopNT) out[i] = 0;
+  write_ranked(list[cur], have, k, out);
+  if (threadIdx.x == 0) ms[blockIdx.x] = make_float2(M, red_s[0] + red_s[1] + red_s[2] + red_s[3]);
+  for (int i = min(have, k) + threadIdx.x; i < k; i += kTopNT) out[i] = 0;
 }
 
 // One workgroup per row joins its parts' lists and log-sum-exps.  A threshold that k
 // candidates reach: the ceil(k / parts)-th of every part, the smallest of them, or the
 // k-th of any one part.
-constexpr int kMergeNT = 256;
+// The candidates are read once, into registers (kMergeHold a thread hold all there
+// can be).
+constexpr int kMergeNT = 256, kMergeWaves = kMergeNT / 64, kMergeHold = 16;
+constexpr int kMaxCand = kMergeNT * kMergeHold;
 template <typename T>
 __global__ __launch_bounds__(kMergeNT) void topk_merge_kernel(const void *logits, int64_t ld,
                                                               int vocab, int parts, int k,
-                                                              double c, const uint64_t *cand,
+                                                              double inv_temp, const uint64_t *cand,
                                                               const float2 *ms, int32_t *idx,
                                                               float *logprob, float *lse) {
-  __shared__ uint64_t list[kTopCap], least[kMergeNT / 64], most[kMergeNT / 64], ranked[kMaxK];
-  __shared__ double red[kMergeNT / 64];
-  __shared__ float red_m[kMergeNT / 64];
-  __shared__ int red_i[kMergeNT / 64], n_list;
+  __shared__ __attribute__((aligned(16))) uint64_t list[kMaxK + kSlack + kRankPad];
+  __shared__ uint64_t least[kMergeWaves], most[kMergeWaves], first[kMergeWaves], ranked[kMaxK];
+  __shared__ double red[kMergeWaves];
+  __shared__ float red_m[kMergeWaves];
+  __shared__ int red_i[3][kMergeWaves], n_list;
+  static_assert(kMergeWaves == kTopWaves, "kth_place's waves");
   const int64_t row = blockIdx.x;
   const uint64_t *in = cand + row * parts * k;
   const float2 *p = ms + row * parts;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_in = parts * k;
+  uint64_t v[kMergeHold];
+#pragma unroll
+  for (int h = 0; h < kMergeHold; ++h) {
+    const int i = h * kMergeNT + threadIdx.x;
+    v[h] = i < n_in ? in[i] : 0;
+  }
   const int j = (k + parts - 1) / parts;
-  uint64_t lo = ~(uint64_t)0, hi = 0;
+  uint64_t lo = ~(uint64_t)0, hi = 0, top = 0;
   float M = -INFINITY;
   for (int q = threadIdx.x; q < parts; q += kMergeNT) {
     lo = min(lo, in[(int64_t)q * k + j - 1]);
     hi = max(hi, in[(int64_t)q * k + k - 1]);
+    top = max(top, in[(int64_t)q * k]);
     M = fmaxf(M, p[q].x);
   }
   lo = ~wave_max(~lo);
   hi = wave_max(hi);
+  top = wave_max(top);
   M = wave_max(M);
   if (threadIdx.x == 0) n_list = 0;
-  if (lane == 0) least[wave] = lo, most[wave] = hi, red_m[wave] = M;
+  if (lane == 0) least[wave] = lo, most[wave] = hi, first[wave] = top, red_m[wave] = M;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kMergeNT / 64; ++w) {
+  for (int w = 0; w < kMergeWaves; ++w) {
     lo = min(lo, least[w]);
     hi = max(hi, most[w]);
+    top = max(top, first[w]);
     M = fmaxf(M, red_m[w]);
   }
-  uint64_t t = max(lo, hi);
+  uint64_t t = max(max(lo, hi), (uint64_t)1);   // (0 is no place)
   // the row's log-sum-exp in 64 bits from the parts' sums
   double s = 0.0;
   for (int q = threadIdx.x; q < parts; q += kMergeNT)
-    s += p[q].x == -INFINITY && p[q].y == 0.f ? 0.0 : (double)p[q].y * exp2(((double)p[q].x - M) * c);
+    s += p[q].x == -INFINITY && p[q].y == 0.f ? 0.0 : (double)p[q].y * exp2((double)p[q].x - M);
   s = wave_sum(s);
   if (lane == 0) red[wave] = s;
-  int cnt = 0;
-  for (int i = threadIdx.x; i < n_in; i += kMergeNT) cnt += in[i] >= t && in[i] != 0;
-  cnt = block_sum(cnt, red_i);
+  __syncthreads();
   s = 0.0;
 #pragma unroll
-  for (int w = 0; w < kMergeNT / 64; ++w) s += red[w];
-  const double l = M == -INFINITY && s == 0.0 ? -INFINITY : (M * c + log2(s)) * kLn2D;
-  if (cnt > kTopCap)
-    t = kth_place(k, red_i, [&](uint64_t v) {
-      int n = 0;
-      for (int i = threadIdx.x; i < n_in; i += kMergeNT) n += in[i] >= v;
-      return n;
-    });
-  for (int i = threadIdx.x; i < n_in; i += kMergeNT)
-    if (in[i] >= t && in[i] != 0) list[atomicAdd(&n_list, 1)] = in[i];
+  for (int w = 0; w < kMergeWaves; ++w) s += red[w];
+  const double l = M == -INFINITY && s == 0.0 ? -INFINITY : (M + log2(s)) * kLn2D;
+  t = kth_place(k, k + kSlack, t, top + 1, red_i, [&](uint64_t p) {
+    int n = 0;
+#pragma unroll
+    for (int h = 0; h < kMergeHold; ++h) n += __popcll(__builtin_amdgcn_ballot_w64(v[h] >= p));
+    return n;
+  });
+#pragma unroll
+  for (int h = 0; h < kMergeHold; ++h)
+    if (v[h] >= t) list[atomicAdd(&n_list, 1)] = v[h];
   __syncthreads();
   write_ranked(list, n_list, k, ranked);
   __syncthreads();
   for (int i = threadIdx.x; i < k; i += kMergeNT) {
-    const int v = (int)~(uint32_t)ranked[i];
-    const double z = ldf((const T *)logits + row * ld + v);
-    idx[row * k + i] = v;
+    const int id = place_index(ranked[i]);
+    const double z = ldf((const T *)logits + row * ld + id);
+    idx[row * k + i] = id;
     // a row of nothing but -inf has no probabilities: -inf for each
-    logprob[row * k + i] = l == -INFINITY ? -INFINITY : (float)(z * (c * kLn2D) - l);
+    logprob[row * k + i] = l == -INFINITY ? -INFINITY : (float)(z * inv_temp - l);
   }
   if (threadIdx.x == 0) lse[row] = (float)l;
 }
@@ -400,8 +558,8 @@ AJ_DEV void mark(uint32_t *bits, int v, int shift, int vocab, int u0, int u1) {
   if (u >= u0 && u < u1) atomicOr(&bits[(u - u0) >> 5], 1u << ((u - u0) & 31));
 }
 
-// One workgroup per part [u0, u1) of a row: maximum and sum of exp2((z - max) c) of the
-// values that the list does not name.
+// One workgroup per part [u0, u1) of a row: the sum of 2^(z c) over the values that the list
+// does not name, as a power of two (log2 units) and a factor.
 template <typename T>
 __global__ __launch_bounds__(kNT) void distill_part_kernel(const void *logits, int64_t ld, int vocab,
                                                            int parts, int width, Teacher t, float c,
@@ -414,16 +572,14 @@ __global__ __launch_bounds__(kNT) void distill_part_kernel(const void *logits, i
   const int u0 = blockIdx.x % parts * width, u1 = min(u0 + width, x.end);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   typename Row<T>::Bits b[kQ];
-  auto fetch = [&](int u) {
-#pragma unroll
-    for (int q = 0; q < kQ; ++q) b[q] = x.load(u + (q * kNT + threadIdx.x) * R);
-  };
+  auto fetch = [&](int u) __attribute__((always_inline)) { x.load(b, u, threadIdx.x * R, kNT * R, kStep); };
   fetch(u0);
   for (int i = threadIdx.x; i < width / 32; i += kNT) bits[i] = 0;
   __syncthreads();
   if ((int)threadIdx.x < t.k) mark(bits, t.idx[row * t.k + threadIdx.x], x.shift, vocab, u0, u1);
   __syncthreads();
-  float m = -INFINITY, s = 0.f;
+  // s counts in units of 2^ref, ref the rounded product of the largest value and c
+  float ref = -INFINITY, s = 0.f;
   for (int u = u0; u < u1; u += kStep) {
     float z[kQ * R];
 #pragma unroll
@@ -431,29 +587,33 @@ __global__ __launch_bounds__(kNT) void distill_part_kernel(const void *logits, i
       float v[R];
       Row<T>::values(b[q], v);
       const int at = u - u0 + (q * kNT + threadIdx.x) * R;
-      uint32_t w = 0;
-      if (u0 + at < u1) w = bits[at >> 5] >> (at & 31);
-      const bool in = u0 + at < u1;
+      // few runs hold a named value, or lie in the next part: the rest skip this whole
+      uint32_t w = at < width ? bits[at >> 5] >> (at & 31) & ((1u << R) - 1) : (1u << R) - 1;
 #pragma unroll
-      for (int j = 0; j < R; ++j) z[q * R + j] = (w >> j & 1) | !in ? -INFINITY : v[j];
+      for (int j = 0; j < R; ++j) z[q * R + j] = v[j];
+      if (__builtin_amdgcn_ballot_w64(w != 0)) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) z[q * R + j] = w >> j & 1 ? -INFINITY : v[j];
+      }
     }
     if (u + kStep < u1) fetch(u + kStep);
-    float n = m;
+    float n = z[0];
 #pragma unroll
-    for (int e = 0; e < kQ * R; ++e) n = fmaxf(n, z[e]);
+    for (int e = 1; e < kQ * R; ++e) n = fmaxf(n, z[e]);
+    n = fmaxf(ref, n * c);
     const float base = n == -INFINITY ? 0.f : n;
-    s *= m == -INFINITY ? 0.f : fast_exp2((m - base) * c);
-    m = n;
+    s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
+    ref = n;
 #pragma unroll
-    for (int e = 0; e < kQ * R; ++e) s += fast_exp2((z[e] - base) * c);
+    for (int e = 0; e < kQ * R; ++e) s += fast_exp2(fmaf(z[e], c, -base));
   }
-  float M = wave_max(m);
-  if (lane == 0) red_m[wave] = M;
+  const float wm = wave_max(ref);
+  if (lane == 0) red_m[wave] = wm;
   __syncthreads();
+  float M = red_m[0];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, red_m[w]);
-  // (0 times an infinity, of a thread that has met +inf, is the NaN it should be)
-  s = wave_sum(m == -INFINITY ? s : s * fast_exp2((m - M) * c));
+  for (int w = 1; w < kWaves; ++w) M = fmaxf(M, red_m[w]);
+  s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - M));
   if (lane == 0) red_s[wave] = s;
   __syncthreads();
   if (threadIdx.x == 0) ms[blockIdx.x] = make_float2(M, red_s[0] + red_s[1] + red_s[2] + red_s[3]);
@@ -486,9 +646,9 @@ __global__ __launch_bounds__(kNT) void distill_row_kernel(const void *logits, in
   M = block_max(M);
   double s = 0.0;
   for (int q = threadIdx.x; q < parts; q += kNT)
-    s += p[q].x == -INFINITY && p[q].y == 0.f ? 0.0 : (double)p[q].y * exp2(((double)p[q].x - M) * c);
+    s += p[q].x == -INFINITY && p[q].y == 0.f ? 0.0 : (double)p[q].y * exp2((double)p[q].x - M);
   s = block_sum(s, red);
-  const double rest = s == 0.0 ? -INFINITY : (M * c + log2(s)) * kLn2D;   // of the others
+  const double rest = s == 0.0 ? -INFINITY : (M + log2(s)) * kLn2D;   // of the others
   const double mz = block_max(z);
   const double sz = block_sum(z == -INFINITY ? 0.0 : exp2((z - mz) * c), red);
   const double list = sz == 0.0 ? -INFINITY : (mz * c + log2(sz)) * kLn2D;
@@ -539,10 +699,7 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
   const Row<T> x(logits, row, ld, vocab);
   const int u0 = blockIdx.x % parts * width, u1 = min(u0 + width, x.end);
   typename Row<T>::Bits b[kQ];
-  auto fetch = [&](int u) {
-#pragma unroll
-    for (int q = 0; q < kQ; ++q) b[q] = x.load(u + (q * kNT + threadIdx.x) * R);
-  };
+  auto fetch = [&](int u) __attribute__((always_inline)) { x.load(b, u, threadIdx.x * R, kNT * R, kStep); };
   fetch(u0);
   const Listed e = listed(t, row, vocab, nullptr, ids, red);
   const double all = lse[row], others = lse[rows + row];
@@ -599,37 +756,31 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
 }
 
 // ------------------------------------------------------------------ host
-// Room for the parts' results is asked for so that a workspace sized for some rows serves
-// fewer: `full` parts a row, or, where small numbers of rows are cut finer (`fine` parts a
-// row at most), the `most` of them that this ever gives.
-size_t part_room(int64_t rows, int64_t full, int64_t fine, int64_t most) {
-  return (size_t)std::max(rows * full, std::min(rows * fine, most));
-}
-
 struct TopWs {
   uint64_t *cand;
   float2 *ms;
-  int parts, per_thread;
+  int parts, width, per_thread;
   size_t bytes;
 };
 
-// Values per thread of the part kernel: 32 (16384 a part); fewer where the rows are
-// too few to give every CU a part.
-int top_per_thread(int rows, int vocab) {
-  int e = 32;
-  while (e > 8 && (int64_t)rows * ((vocab + kTopNT * e - 1) / (kTopNT * e)) < 256) e /= 2;
-  return e;
-}
-
+// Parts of a row: 4096 workgroups in all where the rows are fewer (four rounds of what
+// the card holds), in multiples of 32 values a thread; where even such parts are under
+// 512, parts of 16 a thread.  Never more than the join holds: candidates of all a row's
+// parts, kMaxCand.
 TopWs carve_top(int rows, int vocab, int k, void *base) {
   aj::Carver cv(base);
   TopWs w;
-  w.per_thread = top_per_thread(rows, vocab);
-  // a row that starts past a run boundary reaches at most 7 values further
-  auto parts = [&](int e) { return (vocab + 7 + kTopNT * e - 1) / (kTopNT * e); };
-  w.parts = parts(w.per_thread);
-  // finer parts are taken from under 256 in all, and at most double them and one a row
-  const size_t room = part_room(rows, parts(32), parts(8), 768);
+  const int64_t span = (int64_t)vocab + 7;   // a row may start 7 values past a run boundary
+  auto chunks = [&](int e) { return (span + kTopNT * e - 1) / (kTopNT * e); };
+  w.per_thread = rows * chunks(32) < 512 ? 16 : 32;
+  const int64_t n = chunks(w.per_thread);
+  int64_t parts = std::min(n, std::max<int64_t>(1, 4096 / std::max(rows, 1)));
+  parts = std::min<int64_t>(parts, kMaxCand / k);
+  w.width = (int)((n + parts - 1) / parts) * kTopNT * w.per_thread;
+  w.parts = (int)((span + w.width - 1) / w.width);
+  // at least what fewer rows, cut finer, ask for
+  const size_t room =
+      (size_t)std::max((int64_t)rows * w.parts, std::min<int64_t>(rows * chunks(16), 4096));
   w.cand = cv.take<uint64_t>(room * k);
   w.ms = cv.take<float2>(room);
   w.bytes = cv.bytes();
@@ -677,13 +828,11 @@ void launch_topk(const aj_logits &lg, int k, int32_t *idx, float *logprob, float
   const float c = lg.inv_temp * kLog2e;
   const unsigned grid = (unsigned)lg.rows * w.parts;
   if (w.per_thread == 32)
-    topk_part_kernel<T, 32><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, k, c, w.cand, w.ms);
-  else if (w.per_thread == 16)
-    topk_part_kernel<T, 16><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, k, c, w.cand, w.ms);
+    topk_part_kernel<T, 32><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, c, w.cand, w.ms);
   else
-    topk_part_kernel<T, 8><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, k, c, w.cand, w.ms);
-  topk_merge_kernel<T><<<lg.rows, kMergeNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, k,
-                                                     lg.inv_temp * kLog2eD, w.cand, w.ms, idx, logprob, lse);
+    topk_part_kernel<T, 16><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, c, w.cand, w.ms);
+  topk_merge_kernel<T><<<lg.rows, kMergeNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, k, lg.inv_temp,
+                                                     w.cand, w.ms, idx, logprob, lse);
 }
 
 template <typename T>
@@ -713,8 +862,8 @@ void launch_grad(const aj_logits &lg, const aj_teacher &t, const float *lse, voi
 size_t distill_ws(int rows, int vocab) {
   auto parts = [&](int width) { return (vocab + 7 + width - 1) / width; };
   aj::Carver cv(nullptr);
-  // (as above: halved from under 2048)
-  cv.take<float2>(part_room(rows, parts(kSplit), parts(2048), 3 * 2048));
+  // at least what fewer rows, cut finer (halved from under 2048 parts), ask for
+  cv.take<float2>(std::max((int64_t)rows * parts(kSplit), std::min<int64_t>((int64_t)rows * parts(2048), 3 * 2048)));
   return cv.bytes();
 }
 
