@@ -132,7 +132,8 @@ AJ_DEV float order_value(uint32_t o) {
 }
 
 constexpr int kTopNT = 256, kTopWaves = kTopNT / 64;
-constexpr int kTopCap = 1024;    // candidates kept in LDS
+constexpr int kWaveHold = 5, kWaveCap = 64 * kWaveHold;    // candidates a wave keeps in LDS
+constexpr int kRankPad = 16;
 constexpr int kSlack = 64;       // over k that a last cut may leave to the ranking
 
 // A threshold in [lo, hi) that kk places reach and no more than `most`, where kk and more
@@ -157,61 +158,122 @@ AJ_DEV uint64_t kth_place(int kk, int most, uint64_t lo, uint64_t hi, int (*red)
   return lo;
 }
 
-// The kk largest of the n places of `in`, of which all reach lo, and some next ones, `most`
-// in all, to `out` (in no order); the return value is a threshold that these reach and
-// no other.
-constexpr int kHold = kTopCap / kTopNT;
-AJ_DEV uint64_t cut(const uint64_t *in, int n, int kk, int most, uint64_t lo, uint64_t *out, int (*red)[kTopWaves],
-                    int *n_out) {
-  uint64_t v[kHold], largest = 0;
-#pragma unroll
-  for (int h = 0; h < kHold; ++h) {
-    const int i = h * kTopNT + threadIdx.x;
-    v[h] = i < n ? in[i] : 0;
-    largest = max(largest, v[h]);
+// Candidates met by a workgroup: a list in LDS per wave, which it alone appends to and cuts,
+// so that no atomic is waited for; n is its own wave's length.
+struct WaveList {
+  uint64_t *at;
+  int n;
+  // those lanes' places that reach `least`; nothing is lost but what is past kWaveCap,
+  // which n tells of
+  AJ_DEV void add(uint64_t p, uint64_t least) {
+    const bool hit = p >= least;
+    const uint64_t b = __builtin_amdgcn_ballot_w64(hit);
+    const int i = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0));
+    if (hit && i < kWaveCap) at[i] = p;
+    n += __popcll(b);
   }
-  const uint32_t top = wave_max((uint32_t)(largest >> kIndexBits));
+  AJ_DEV uint64_t get(int h) const {
+    const int i = h * 64 + (threadIdx.x & 63);
+    return i < n ? at[i] : 0;
+  }
+  AJ_DEV void keep(uint64_t least) {
+    uint64_t v[kWaveHold];
+#pragma unroll
+    for (int h = 0; h < kWaveHold; ++h) v[h] = get(h);
+    n = 0;
+#pragma unroll
+    for (int h = 0; h < kWaveHold; ++h) add(v[h], least);
+  }
+};
+
+// The sum over the waves of what each gives (the barrier also ends what they did in LDS).
+AJ_DEV int waves_sum(int v, int *red) {
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   lds_barrier();
-  if (threadIdx.x == 0) *n_out = 0;
-  if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = (int)top;
+  return __builtin_amdgcn_readfirstlane(red[0] + red[1] + red[2] + red[3]);
+}
+
+// Cuts the lists to the kk largest of their places, of which all reach lo, and some next
+// ones, `most` in all; the return value is a threshold that these reach and no other.
+AJ_DEV uint64_t cut(WaveList &l, int kk, int most, uint64_t lo, int (*red)[kTopWaves]) {
+  uint64_t v[kWaveHold];
+  uint32_t largest = 0;
+#pragma unroll
+  for (int h = 0; h < kWaveHold; ++h) {
+    v[h] = l.get(h);
+    largest = max(largest, (uint32_t)(v[h] >> kIndexBits));
+  }
+  largest = wave_max(largest);
+  lds_barrier();
+  if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = (int)largest;
   lds_barrier();
   uint32_t hi = 0;
 #pragma unroll
   for (int w = 0; w < kTopWaves; ++w) hi = max(hi, (uint32_t)red[0][w]);
   hi = __builtin_amdgcn_readfirstlane(hi);
-  const uint64_t t = kth_place(kk, most, max(lo, (uint64_t)1), (uint64_t)(hi + 1) << kIndexBits, red, [&](uint64_t p) {
+  const uint64_t t = kth_place(kk, most, max(lo, (uint64_t)1), (uint64_t)(hi + 1) << kIndexBits, red,
+                               [&](uint64_t p) {
     int c = 0;
 #pragma unroll
-    for (int h = 0; h < kHold; ++h) c += __popcll(__builtin_amdgcn_ballot_w64(v[h] >= p));
+    for (int h = 0; h < kWaveHold; ++h) c += __popcll(__builtin_amdgcn_ballot_w64(v[h] >= p));
     return c;
   });
+  l.n = 0;
 #pragma unroll
-  for (int h = 0; h < kHold; ++h)
-    if (v[h] >= t) out[atomicAdd(n_out, 1)] = v[h];
-  lds_barrier();
+  for (int h = 0; h < kWaveHold; ++h) l.add(v[h], t);
   return t;
 }
 
-// Largest to smallest: out[r] = the place with r larger ones among the n of c (LDS, room
-// for kRankPad more), r < kk.  Every thread counts for a candidate of its own, 16 of the
-// others at a time: as many LDS reads in flight cover each other's latency (one at a time
-// took 5 us of 200 candidates).  The time goes with n^2, so longer lists are cut first.
-constexpr int kRankPad = 16;
-AJ_DEV void write_ranked(uint64_t *c, int n, int kk, uint64_t *out) {
-  if (threadIdx.x < kRankPad) c[n + threadIdx.x] = 0;
+// Largest to smallest: out[r] (LDS) = the place with r larger ones in the waves' lists, r < kk.
+// Every thread counts for candidates of its own, 16 of the others at a time: as many LDS
+// reads in flight cover each other's latency.  The time goes with the square of the
+// number, so longer lists are cut first.
+AJ_DEV void write_ranked(const WaveList &l, uint64_t (*lists)[kWaveCap + kRankPad], int kk, uint64_t *out,
+                         int *red) {
+  const int lane = threadIdx.x & 63;
+  if (lane < kRankPad) l.at[l.n + lane] = 0;
   lds_barrier();
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const uint64_t mine = c[i];
-    int r = 0;
+  waves_sum(l.n, red);
+  int r[kWaveHold] = {};
+  uint64_t mine[kWaveHold];
+#pragma unroll
+  for (int h = 0; h < kWaveHold; ++h) mine[h] = l.get(h);
+  for (int w = 0; w < kTopWaves; ++w) {
+    const int n = __builtin_amdgcn_readfirstlane(red[w]);
     for (int j = 0; j < n; j += kRankPad) {
       ulonglong2 v[kRankPad / 2];
 #pragma unroll
-      for (int q = 0; q < kRankPad / 2; ++q) v[q] = *reinterpret_cast<const ulonglong2 *>(c + j + 2 * q);
+      for (int q = 0; q < kRankPad / 2; ++q) v[q] = *reinterpret_cast<const ulonglong2 *>(lists[w] + j + 2 * q);
 #pragma unroll
-      for (int q = 0; q < kRankPad / 2; ++q) r += (int)(v[q].x > mine) + (int)(v[q].y > mine);
+      for (int h = 0; h < kWaveHold; ++h) {
+        if (h * 64 >= l.n) break;
+#pragma unroll
+        for (int q = 0; q < kRankPad / 2; ++q) r[h] += (int)(v[q].x > mine[h]) + (int)(v[q].y > mine[h]);
+      }
     }
-    if (r < kk) out[r] = mine;
   }
+#pragma unroll
+  for (int h = 0; h < kWaveHold; ++h)
+    if (h * 64 + lane < l.n && r[h] < kk) out[r[h]] = mine[h];
+}
+
+// A row's results from its k largest places and its log-sum-exp.
+template <typename T>
+AJ_DEV void write_row(const void *logits, int64_t ld, int64_t row, int k, double inv_temp, const uint64_t *ranked,
+                      double l, int32_t *idx, float *logprob, float *lse) {
+  const int i = threadIdx.x;
+  if (i < k) {
+    const int id = place_index(ranked[i]);
+    const double z = ldf((const T *)logits + row * ld + id);
+    idx[row * k + i] = id;
+    // a row of nothing but -inf has no probabilities: -inf for each
+    logprob[row * k + i] = l == -INFINITY ? -INFINITY : (float)(z * inv_temp - l);
+  }
+  if (i == 0) lse[row] = (float)l;
+}
+// natural log of a sum given as a power of two and a factor
+AJ_DEV double log_of(double power, double sum) {
+  return power == -INFINITY && sum == 0.0 ? -INFINITY : (power + log2(sum)) * kLn2D;
 }
 
 // One workgroup per part [u0, u0 + width) of a row, kTopNT * E values at a time, the next
@@ -227,13 +289,15 @@ AJ_DEV void write_ranked(uint64_t *c, int n, int kk, uint64_t *out) {
 // which is never below), a bisection over the places finds the k-th itself.
 template <typename T, int E>
 __global__ __launch_bounds__(kTopNT, E == 32 ? 4 : 5) void topk_part_kernel(
-    const void *logits, int64_t ld, int vocab, int parts, int width, int k, float c, uint64_t *cand,
-    float2 *ms) {
+    const void *logits, int64_t ld, int vocab, int parts, int width, int k, float inv_temp, uint64_t *cand,
+    float2 *ms, int32_t *idx, float *logprob, float *lse) {
   constexpr int R = kRun<T>, Q = E / R, C = kTopNT * E;
-  __shared__ __attribute__((aligned(16))) uint64_t list[2][kTopCap + kRankPad];
+  __shared__ __attribute__((aligned(16))) uint64_t lists[kTopWaves][kWaveCap + kRankPad];
+  __shared__ uint64_t ranked[kMaxK];
   __shared__ float red_m[kTopWaves], red_s[kTopWaves];
   __shared__ uint32_t red_t[kTopWaves];
-  __shared__ int red_i[3][kTopWaves], added[3], n_kept;
+  __shared__ int red_i[3][kTopWaves], red_n[3][kTopWaves];
+  const float c = inv_temp * kLog2e;
   const int64_t row = blockIdx.x / parts;
   const int part = blockIdx.x % parts;
   const Row<T> x(logits, row, ld, vocab);
@@ -254,9 +318,8 @@ __global__ __launch_bounds__(kTopNT, E == 32 ? 4 : 5) void topk_part_kernel(
   // the row's rim goes with its first part, a value for each of some threads
   const int rim = part == 0 && threadIdx.x < 2 * R ? x.rim(threadIdx.x) : -1;
   const float zr = rim >= 0 ? ldf(x.aligned + rim) : -INFINITY;
-  if (threadIdx.x < 3) added[threadIdx.x] = 0;
-  int cur = 0, have = 0;      // the list in use and what it holds
-  uint64_t least = 0;         // the least place that goes to it
+  WaveList list{lists[wave], 0};
+  uint64_t least = 0;         // the least place that goes to a list
   float tau = -INFINITY;      // ... and its value
   float ref = -INFINITY, s = 0.f;
   int turn = 0;
@@ -281,9 +344,9 @@ __global__ __launch_bounds__(kTopNT, E == 32 ? 4 : 5) void topk_part_kernel(
       else m0 = fmaxf(m0, top[q]);
     }
     // s counts in units of 2^ref, ref the rounded product of the largest value and c
-    const float n = fmaxf(ref, fmaxf(m0, m1) * c), base = n == -INFINITY ? 0.f : n;
+    const float up = fmaxf(ref, fmaxf(m0, m1) * c), base = up == -INFINITY ? 0.f : up;
     s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
-    ref = n;
+    ref = up;
 #pragma unroll
     for (int e = 0; e < E; ++e) s += fast_exp2(fmaf(z[e], c, -base));
     if (first) {
@@ -315,77 +378,64 @@ __global__ __launch_bounds__(kTopNT, E == 32 ? 4 : 5) void topk_part_kernel(
       const int ur = v - e % R + x.shift;      // its run; the rim is not among them
       return ur >= x.shift && ur + R <= x.end ? place(ze, v) : 0;
     };
-    auto add = [&](uint64_t p) {
-      if (p < least || p == 0) return;
-      const int at = have + atomicAdd(&added[turn], 1);
-      if (at < kTopCap) list[cur][at] = p;
-    };
+    const uint64_t pr = first && rim >= 0 ? place(zr, rim - x.shift) : 0;
     // a thread whose sum is NaN has met a NaN (which no maximum shows) or +inf: it
     // looks at all it holds
     float bar = s == s ? tau : -INFINITY;
+    int had = list.n, n;
     for (;;) {
 #pragma unroll
       for (int q = 0; q < Q; ++q)
         if (__builtin_amdgcn_ballot_w64(!(top[q] < bar))) {
 #pragma unroll
-          for (int j = 0; j < R; ++j) add(place_of(q * R + j));
+          for (int j = 0; j < R; ++j)
+            if (__builtin_amdgcn_ballot_w64(!(z[q * R + j] < bar))) list.add(place_of(q * R + j), max(least, (uint64_t)1));
         }
-      if (first && rim >= 0) add(place(zr, rim - x.shift));
-      // (the next turn's counter was last read two turns ago)
-      const int now = turn;
+      if (first) list.add(pr, max(least, (uint64_t)1));
+      // (a list that is too long counts for more than all may hold)
+      n = waves_sum(list.n > kWaveCap ? kTopWaves * kWaveCap + 1 : list.n, red_n[turn]);
       turn = turn == 2 ? 0 : turn + 1;
-      if (threadIdx.x == 0) added[turn] = 0;
-      lds_barrier();
-      const int n_list = have + added[now];
-      if (n_list <= kTopCap) {
-        have = n_list;
-        break;
-      }
-      // too many: again with the k-th place of the list as it was and these values
-      auto count = [&](uint64_t p) {
-        int cnt = 0;
-        for (int i = 0; i < have; i += kTopNT)
-          cnt += __popcll(__builtin_amdgcn_ballot_w64(i + (int)threadIdx.x < have &&
-                                                      list[cur][i + threadIdx.x] >= p));
+      if (n <= kTopWaves * kWaveCap) break;
+      // too many: again with the k-th place of the lists as they were and these values
+      list.n = had;
+      least = kth_place(k, k, 1, kAbove, red_i, [&](uint64_t p) {
+        int cnt = __popcll(__builtin_amdgcn_ballot_w64(pr >= p));
+#pragma unroll
+        for (int h = 0; h < kWaveHold; ++h) cnt += __popcll(__builtin_amdgcn_ballot_w64(list.get(h) >= p));
 #pragma unroll
         for (int e = 0; e < E; ++e) cnt += __popcll(__builtin_amdgcn_ballot_w64(place_of(e) >= p));
-        if (first)
-          cnt += __popcll(__builtin_amdgcn_ballot_w64(rim >= 0 && place(zr, rim - x.shift) >= p));
         return cnt;
-      };
-      least = kth_place(k, k, 1, kAbove, red_i, count);
+      });
+      list.keep(least);
+      had = list.n;
+      tau = order_value((uint32_t)(least >> kIndexBits));
       bar = -INFINITY;
-      if (threadIdx.x == 0) n_kept = 0;
-      lds_barrier();
-      for (int i = threadIdx.x; i < have; i += kTopNT)
-        if (list[cur][i] >= least) list[cur ^ 1][atomicAdd(&n_kept, 1)] = list[cur][i];
-      lds_barrier();
-      have = __builtin_amdgcn_readfirstlane(n_kept);
-      cur ^= 1;
-      tau = order_value((uint32_t)(least >> kIndexBits));
     }
-    if (have >= 2 * k + 64 && u + C < u1) {
-      least = cut(list[cur], have, k, k + k / 4 + 32, least, list[cur ^ 1], red_i, &n_kept);
-      cur ^= 1;
-      have = __builtin_amdgcn_readfirstlane(n_kept);
+    if (n >= 2 * k + 64 && u + C < u1) {
+      least = cut(list, k, k + k / 4 + 32, least, red_i);
       tau = order_value((uint32_t)(least >> kIndexBits));
     }
   }
-  if (have > k + 128) {
-    cut(list[cur], have, k, k + kSlack, least, list[cur ^ 1], red_i, &n_kept);
-    cur ^= 1;
-    have = __builtin_amdgcn_readfirstlane(n_kept);
-  }
+  // (the barrier ends the reads of this turn's sum)
+  lds_barrier();
+  const int n = waves_sum(list.n, red_n[0]);
+  if (n > k + 128) cut(list, k, k + kSlack, least, red_i);
   const float wm = wave_max(ref);
   if (lane == 0) red_m[wave] = wm;
   __syncthreads();
   const float M = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
   s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - M));
   if (lane == 0) red_s[wave] = s;
-  uint64_t *out = cand + (int64_t)blockIdx.x * k;
-  write_ranked(list[cur], have, k, out);
-  if (threadIdx.x == 0) ms[blockIdx.x] = make_float2(M, red_s[0] + red_s[1] + red_s[2] + red_s[3]);
-  for (int i = min(have, k) + threadIdx.x; i < k; i += kTopNT) out[i] = 0;
+  if ((int)threadIdx.x < k) ranked[threadIdx.x] = 0;
+  write_ranked(list, lists, k, ranked, red_i[0]);
+  __syncthreads();
+  const float S = red_s[0] + red_s[1] + red_s[2] + red_s[3];
+  if (parts == 1) {
+    write_row<T>(logits, ld, row, k, inv_temp, ranked, log_of(M, S), idx, logprob, lse);
+    return;
+  }
+  if ((int)threadIdx.x < k) cand[(int64_t)blockIdx.x * k + threadIdx.x] = ranked[threadIdx.x];
+  if (threadIdx.x == 0) ms[blockIdx.x] = make_float2(M, S);
 }
 
 // One workgroup per row joins its parts' lists and log-sum-exps.  A threshold that k
@@ -401,12 +451,12 @@ __global__ __launch_bounds__(kMergeNT) void topk_merge_kernel(const void *logits
                                                               double inv_temp, const uint64_t *cand,
                                                               const float2 *ms, int32_t *idx,
                                                               float *logprob, float *lse) {
-  __shared__ __attribute__((aligned(16))) uint64_t list[kMaxK + kSlack + kRankPad];
+  __shared__ __attribute__((aligned(16))) uint64_t lists[kTopWaves][kWaveCap + kRankPad];
   __shared__ uint64_t least[kMergeWaves], most[kMergeWaves], first[kMergeWaves], ranked[kMaxK];
   __shared__ double red[kMergeWaves];
   __shared__ float red_m[kMergeWaves];
-  __shared__ int red_i[3][kMergeWaves], n_list;
-  static_assert(kMergeWaves == kTopWaves, "kth_place's waves");
+  __shared__ int red_i[3][kMergeWaves];
+  static_assert(kMergeWaves == kTopWaves && kMaxK + kSlack <= kWaveCap, "the waves' lists");
   const int64_t row = blockIdx.x;
   const uint64_t *in = cand + row * parts * k;
   const float2 *p = ms + row * parts;
@@ -430,7 +480,6 @@ __global__ __launch_bounds__(kMergeNT) void topk_merge_kernel(const void *logits
   hi = wave_max(hi);
   top = wave_max(top);
   M = wave_max(M);
-  if (threadIdx.x == 0) n_list = 0;
   if (lane == 0) least[wave] = lo, most[wave] = hi, first[wave] = top, red_m[wave] = M;
   __syncthreads();
 #pragma unroll
@@ -451,27 +500,19 @@ __global__ __launch_bounds__(kMergeNT) void topk_merge_kernel(const void *logits
   s = 0.0;
 #pragma unroll
   for (int w = 0; w < kMergeWaves; ++w) s += red[w];
-  const double l = M == -INFINITY && s == 0.0 ? -INFINITY : (M + log2(s)) * kLn2D;
   t = kth_place(k, k + kSlack, t, top + 1, red_i, [&](uint64_t p) {
     int n = 0;
 #pragma unroll
     for (int h = 0; h < kMergeHold; ++h) n += __popcll(__builtin_amdgcn_ballot_w64(v[h] >= p));
     return n;
   });
+  WaveList list{lists[wave], 0};
 #pragma unroll
-  for (int h = 0; h < kMergeHold; ++h)
-    if (v[h] >= t) list[atomicAdd(&n_list, 1)] = v[h];
+  for (int h = 0; h < kMergeHold; ++h) list.add(v[h], t);
+  lds_barrier();
+  write_ranked(list, lists, k, ranked, red_i[0]);
   __syncthreads();
-  write_ranked(list, n_list, k, ranked);
-  __syncthreads();
-  for (int i = threadIdx.x; i < k; i += kMergeNT) {
-    const int id = place_index(ranked[i]);
-    const double z = ldf((const T *)logits + row * ld + id);
-    idx[row * k + i] = id;
-    // a row of nothing but -inf has no probabilities: -inf for each
-    logprob[row * k + i] = l == -INFINITY ? -INFINITY : (float)(z * inv_temp - l);
-  }
-  if (threadIdx.x == 0) lse[row] = (float)l;
+  write_row<T>(logits, ld, row, k, inv_temp, ranked, log_of(M, s), idx, logprob, lse);
 }
 
 // ------------------------------------------------------------------ distillation
@@ -825,13 +866,15 @@ Teacher teacher_of(const aj_teacher &t) {
 template <typename T>
 void launch_topk(const aj_logits &lg, int k, int32_t *idx, float *logprob, float *lse, const TopWs &w,
                  hipStream_t st) {
-  const float c = lg.inv_temp * kLog2e;
   const unsigned grid = (unsigned)lg.rows * w.parts;
   if (w.per_thread == 32)
-    topk_part_kernel<T, 32><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, c, w.cand, w.ms);
+    topk_part_kernel<T, 32><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, lg.inv_temp,
+                                                     w.cand, w.ms, idx, logprob, lse);
   else
-    topk_part_kernel<T, 16><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, c, w.cand, w.ms);
-  topk_merge_kernel<T><<<lg.rows, kMergeNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, k, lg.inv_temp,
+    topk_part_kernel<T, 16><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, lg.inv_temp,
+                                                     w.cand, w.ms, idx, logprob, lse);
+  if (w.parts > 1)
+    topk_merge_kernel<T><<<lg.rows, kMergeNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, k, lg.inv_temp,
                                                      w.cand, w.ms, idx, logprob, lse);
 }
 
