@@ -7,6 +7,7 @@
 // so that every thread's run of 16 bytes is aligned and only the row's first and last runs
 // are guarded value by value.
 #include <algorithm>
+#include <type_traits>
 #include "ops.h"
 
 namespace {
@@ -536,17 +537,28 @@ struct Listed {
   double mass, rest;   // of the whole row: sum of p and what is left of 1 (tail 1)
 };
 
-AJ_DEV double block_sum(double v, double *red) {
+template <int WAVES> AJ_DEV double block_sum(double v, double *red) {
   v = wave_sum(v);
-  __syncthreads();
+  lds_barrier();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
+  lds_barrier();
   double s = 0.0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) s += red[w];
+  for (int w = 0; w < WAVES; ++w) s += red[w];
   return s;
 }
+template <int WAVES> AJ_DEV double block_max(double v, double *red) {
+  v = wave_max(v);
+  lds_barrier();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  lds_barrier();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) v = max(v, red[w]);
+  return v;
+}
 
+// (threads past the k-th hold nothing; the entries sit in the first kMaxK threads)
+template <int WAVES>
 AJ_DEV Listed listed(const Teacher &t, int64_t row, int vocab, int32_t *err, int *ids, double *red) {
   const int i = threadIdx.x;
   Listed e;
@@ -556,9 +568,9 @@ AJ_DEV Listed listed(const Teacher &t, int64_t row, int vocab, int32_t *err, int
   if (i < t.k) {
     raw = t.idx[row * t.k + i];
     lp = t.logprob[row * t.k + i];
+    ids[i] = raw;
   }
-  ids[i] = raw;
-  __syncthreads();
+  lds_barrier();
   if (raw >= vocab) {
     if (err) atomicOr(err, AJ_DEVERR_TOKEN_RANGE);
   } else if (raw >= 0) {
@@ -570,26 +582,89 @@ AJ_DEV Listed listed(const Teacher &t, int64_t row, int vocab, int32_t *err, int
   if (e.v < 0) lp = -INFINITY;
   if (t.tail) {
     e.logp = lp;
-    e.p = exp(lp);
-    e.mass = block_sum(e.p, red);
+    e.p = lp == -INFINITY ? 0.0 : exp(lp);
+    e.mass = block_sum<WAVES>(e.p, red);
     // (a NaN stays one)
     e.rest = e.mass > 1.0 ? 0.0 : 1.0 - e.mass;
     e.mass += e.rest;
   } else {
-    double m = wave_max(lp);
-    __syncthreads();
-    if ((i & 63) == 0) red[i >> 6] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = max(m, red[w]);
+    const double m = block_max<WAVES>(lp, red);
     const double ex = lp == -INFINITY ? 0.0 : exp(lp - m);
-    const double s = block_sum(ex, red);
+    const double s = block_sum<WAVES>(ex, red);
     e.p = s == 0.0 ? 0.0 : ex / s;
     e.logp = lp - m - log(s);
     e.mass = s == 0.0 ? 0.0 : 1.0;
     e.rest = 0.0;
   }
   return e;
+}
+
+// What a row's loss and gradient come from: log-sum-exps of the whole row and of the
+// values not named, and the loss.
+struct RowSums { double all, rest, loss; };
+// ms (parts of them): the others' sums as powers of two and factors; z: this thread's named value
+template <int WAVES>
+AJ_DEV RowSums row_sums(const Listed &e, double z, double inv_temp, const float2 *ms, int parts, double *red) {
+  RowSums r;
+  const double c = inv_temp * kLog2eD;
+  double M = -INFINITY;
+  for (int q = threadIdx.x; q < parts; q += 64 * WAVES) M = max(M, (double)ms[q].x);
+  M = block_max<WAVES>(M, red);
+  double s = 0.0;
+  for (int q = threadIdx.x; q < parts; q += 64 * WAVES)
+    s += ms[q].x == -INFINITY && ms[q].y == 0.f ? 0.0 : (double)ms[q].y * exp2((double)ms[q].x - M);
+  s = block_sum<WAVES>(s, red);
+  r.rest = log_of(M, s);
+  const double mz = block_max<WAVES>(z, red);
+  const double sz = block_sum<WAVES>(z == -INFINITY ? 0.0 : exp2((z - mz) * c), red);
+  const double list = sz == 0.0 ? -INFINITY : (mz * c + log2(sz)) * kLn2D;
+  const double hi = max(r.rest, list);
+  r.all = r.rest + list;     // NaN where one is
+  if (r.all == r.all || hi == -INFINITY)
+    r.all = hi == -INFINITY ? -INFINITY : hi + log(exp(r.rest - hi) + exp(list - hi));
+  double term = 0.0;
+  if (e.p > 0.0 || e.p != e.p) term = e.p * (e.logp - (z * inv_temp - r.all));
+  r.loss = block_sum<WAVES>(term, red);
+  if (e.rest > 0.0) r.loss += e.rest * (log(e.rest) - (r.rest - r.all));
+  return r;
+}
+
+// The gradient of the values not named, 2^(z c - ref) f, and of a named one.
+struct RowGrad {
+  float c, ref, f;
+  double w;
+  AJ_DEV RowGrad(const Teacher &t, const Listed &e, double inv_temp, double weight, double all, double rest) {
+    w = (double)t.coef * inv_temp * weight;
+    const double l = t.tail ? rest : all;
+    ref = l == -INFINITY ? 0.f : (float)(l * kLog2eD);
+    c = (float)(inv_temp * kLog2eD);
+    f = (float)(t.tail ? w * (e.mass * exp(rest - all) - e.rest) : w * e.mass);
+    if (e.mass == 0.0) f = 0.f;
+    none = e.mass == 0.0;
+  }
+  bool none;      // nothing listed: no loss, no gradient, whatever the logits
+  AJ_DEV float other(float z) const { return none ? 0.f : fast_exp2(fmaf(z, c, -ref)) * f; }
+  AJ_DEV float named(const Listed &e, double z, double inv_temp, double all) const {
+    return none ? 0.f : (float)(w * (e.mass * exp(z * inv_temp - all) - e.p));
+  }
+};
+
+// Stores a run's gradients at out + u (whole: the run lies in the row and out is aligned as
+// it is).
+template <typename G, int R> AJ_DEV void store_run(G *out, const float (&g)[R]) {
+  if constexpr (sizeof(G) == 4) {
+#pragma unroll
+    for (int j = 0; j < R; j += 4)
+      *reinterpret_cast<float4 *>(out + j) = make_float4(g[j], g[j + 1], g[j + 2], g[j + 3]);
+  } else if constexpr (R == 4) {
+    *reinterpret_cast<uint2 *>(out) = make_uint2(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]));
+  } else {
+    *reinterpret_cast<uint4 *>(out) =
+        make_uint4(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]), f2bf2(g[4], g[5]), f2bf2(g[6], g[7]));
+  }
+}
+template <typename G, int R> AJ_DEV bool runs_aligned(const G *out) {
+  return ((uintptr_t)out & (R * sizeof(G) - 1)) == 0 || ((uintptr_t)out & 15) == 0;
 }
 
 // One bit per value of u in [u0, u0 + kSplit): whether the list names it.
@@ -666,45 +741,16 @@ __global__ __launch_bounds__(kNT) void distill_row_kernel(const void *logits, in
                                                           int rows, int parts, Teacher t, double inv_temp,
                                                           const float2 *ms, float *loss, float *lse,
                                                           int32_t *err) {
-  __shared__ int ids[kNT];
+  __shared__ int ids[kMaxK];
   __shared__ double red[kWaves];
   const int64_t row = blockIdx.x;
-  const Listed e = listed(t, row, vocab, err, ids, red);
-  const double c = inv_temp * kLog2eD;
+  const Listed e = listed<kWaves>(t, row, vocab, err, ids, red);
   const double z = e.v >= 0 ? (double)ldf((const T *)logits + row * ld + e.v) : -INFINITY;
-  const float2 *p = ms + row * parts;
-  double M = -INFINITY;
-  for (int q = threadIdx.x; q < parts; q += kNT) M = max(M, (double)p[q].x);
-  auto block_max = [&](double v) {
-    v = wave_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) v = max(v, red[w]);
-    return v;
-  };
-  M = block_max(M);
-  double s = 0.0;
-  for (int q = threadIdx.x; q < parts; q += kNT)
-    s += p[q].x == -INFINITY && p[q].y == 0.f ? 0.0 : (double)p[q].y * exp2((double)p[q].x - M);
-  s = block_sum(s, red);
-  const double rest = s == 0.0 ? -INFINITY : (M + log2(s)) * kLn2D;   // of the others
-  const double mz = block_max(z);
-  const double sz = block_sum(z == -INFINITY ? 0.0 : exp2((z - mz) * c), red);
-  const double list = sz == 0.0 ? -INFINITY : (mz * c + log2(sz)) * kLn2D;
-  const double hi = max(rest, list);
-  double all = rest + list;     // NaN where one is
-  if (all == all || hi == -INFINITY)
-    all = hi == -INFINITY ? -INFINITY : hi + log(exp(rest - hi) + exp(list - hi));
-  double term = 0.0;
-  if (e.p > 0.0 || e.p != e.p) term = e.p * (e.logp - (z * inv_temp - all));
-  term = block_sum(term, red);
-  if (t.tail && e.rest > 0.0) term += e.rest * (log(e.rest) - (rest - all));
+  const RowSums r = row_sums<kWaves>(e, z, inv_temp, ms + row * parts, parts, red);
   if (threadIdx.x == 0) {
-    loss[row] = (float)term;
-    lse[row] = (float)all;
-    lse[rows + row] = (float)rest;
+    loss[row] = (float)r.loss;
+    lse[row] = (float)r.all;
+    lse[rows + row] = (float)r.rest;
   }
 }
 
@@ -734,7 +780,7 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
                                                           double inv_temp, const float *lse, G *dz,
                                                           int64_t ldd) {
   constexpr int R = kRun<T>, kStep = kNT * R * kQ;
-  __shared__ int ids[kNT];
+  __shared__ int ids[kMaxK];
   __shared__ double red[kWaves];
   const int64_t row = blockIdx.x / parts;
   const Row<T> x(logits, row, ld, vocab);
@@ -742,31 +788,23 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
   typename Row<T>::Bits b[kQ];
   auto fetch = [&](int u) __attribute__((always_inline)) { x.load(b, u, threadIdx.x * R, kNT * R, kStep); };
   fetch(u0);
-  const Listed e = listed(t, row, vocab, nullptr, ids, red);
+  const Listed e = listed<kWaves>(t, row, vocab, nullptr, ids, red);
   const double all = lse[row], others = lse[rows + row];
-  const double w = (double)t.coef * inv_temp * (t.weight ? t.weight[row] : 1.f);
+  const RowGrad grad(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, all, others);
   // this part's named values, read before any is written (d logits may be the logits)
   const bool mine = e.v >= 0 && e.v + x.shift >= u0 && e.v + x.shift < u1;
-  float named = 0.f;
-  if (mine) {
-    const double z = ldf((const T *)logits + row * ld + e.v);
-    named = e.mass == 0.0 ? 0.f : (float)(w * (e.mass * exp(z * inv_temp - all) - e.p));
-  }
+  const float named = mine ? grad.named(e, ldf((const T *)logits + row * ld + e.v), inv_temp, all) : 0.f;
   __syncthreads();
-  const double L = t.tail ? others : all;
-  const float L2 = L == -INFINITY ? 0.f : (float)(L * kLog2eD), c = (float)(inv_temp * kLog2eD);
-  const float F = (float)(t.tail ? w * (e.mass * exp(others - all) - e.rest) : w * e.mass);
-  const bool none = e.mass == 0.0;     // nothing listed: no loss, no gradient
   G *out = dz + row * ldd - x.shift;
   // runs are stored whole where d logits is aligned as the runs are
-  const bool vec = ((uintptr_t)out & (R * sizeof(G) - 1)) == 0 || ((uintptr_t)out & 15) == 0;
+  const bool vec = runs_aligned<G, R>(out);
   for (int u = u0; u < u1; u += kStep) {
     float g[kQ][R];
 #pragma unroll
     for (int q = 0; q < kQ; ++q) {
       Row<T>::values(b[q], g[q]);
 #pragma unroll
-      for (int j = 0; j < R; ++j) g[q][j] = none ? 0.f : fast_exp2(fmaf(g[q][j], c, -L2)) * F;
+      for (int j = 0; j < R; ++j) g[q][j] = grad.other(g[q][j]);
     }
     if (u + kStep < u1) fetch(u + kStep);
 #pragma unroll
@@ -774,17 +812,7 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
       const int at = u + (q * kNT + threadIdx.x) * R;
       if (at >= u1) continue;
       if (vec && at >= x.shift && at + R <= x.end) {
-        if constexpr (sizeof(G) == 4) {
-#pragma unroll
-          for (int j = 0; j < R; j += 4)
-            *reinterpret_cast<float4 *>(out + at + j) = make_float4(g[q][j], g[q][j + 1], g[q][j + 2], g[q][j + 3]);
-        } else if constexpr (R == 4) {
-          *reinterpret_cast<uint2 *>(out + at) = make_uint2(f2bf2(g[q][0], g[q][1]), f2bf2(g[q][2], g[q][3]));
-        } else {
-          *reinterpret_cast<uint4 *>(out + at) =
-              make_uint4(f2bf2(g[q][0], g[q][1]), f2bf2(g[q][2], g[q][3]), f2bf2(g[q][4], g[q][5]),
-                         f2bf2(g[q][6], g[q][7]));
-        }
+        store_run<G, R>(out + at, g[q]);
       } else {
 #pragma unroll
         for (int j = 0; j < R; ++j)
@@ -794,6 +822,162 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
   }
   __syncthreads();    // the named ones over what the runs left there
   if (mine) stf(out + e.v + x.shift, named);
+}
+
+// Loss and gradient of a row in one go: one workgroup of 16 waves per row keeps what it
+// reads for the loss on the chip, in registers (kHoldReg runs a thread) and LDS
+// (kHoldLds), and forms the gradient from there; of a float32 row of 152064 values that
+// is 62 %, the rest is read again, newest first, while the caches still have it, and a
+// bfloat16 row of that length is kept whole.
+constexpr int kStepNT = 1024, kStepWaves = kStepNT / 64;
+constexpr int kHoldReg = 12, kHoldLds = 7, kBitWords = 8192;    // 16 KB a run; 32 KB of bits
+constexpr int kStepVocab = kBitWords * 32 - 16;
+template <typename T, typename G>
+__global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logits, int64_t ld, int vocab,
+                                                               int rows, Teacher t, double inv_temp,
+                                                               float *loss, float *lse, int32_t *err, G *dz,
+                                                               int64_t ldd) {
+  constexpr int R = kRun<T>, C = kStepNT * R, NR = sizeof(T) == 4 ? kHoldReg : 8;
+  __shared__ __attribute__((aligned(16))) uint4 held[kHoldLds][kStepNT];
+  __shared__ uint32_t bits[kBitWords];
+  __shared__ int ids[kMaxK];
+  __shared__ double red[kStepWaves];
+  __shared__ float red_m[kStepWaves], red_s[kStepWaves];
+  __shared__ float2 sum;
+  const int64_t row = blockIdx.x;
+  const Row<T> x(logits, row, ld, vocab);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, me = threadIdx.x * R;
+  const int stripes = (x.end + C - 1) / C;
+  typedef typename Row<T>::Bits Bits;
+  auto fetch = [&](int k) __attribute__((always_inline)) { return x.whole(k * C + me); };
+  Bits b[NR];
+#pragma unroll
+  for (int k = 0; k < NR; ++k) b[k] = fetch(k);
+  const int rim = threadIdx.x < 2 * R ? x.rim(threadIdx.x) : -1;
+  const float zr = rim >= 0 ? ldf(x.aligned + rim) : -INFINITY;
+  for (int i = threadIdx.x; i <= x.end / 32; i += kStepNT) bits[i] = 0;
+  const Listed e = listed<kStepWaves>(t, row, vocab, err, ids, red);
+  const double z = e.v >= 0 ? (double)ldf((const T *)logits + row * ld + e.v) : -INFINITY;
+  mark(bits, e.v, x.shift, vocab, 0, x.end);
+  lds_barrier();
+  float ref = -INFINITY, s = 0.f;
+  // adds the values of N runs, at stripes k0, k0 + 1 and so on, that are not named
+  auto absorb = [&](auto N, const Bits *v, int k0) __attribute__((always_inline)) {
+    constexpr int n = decltype(N)::value;
+    float z[n * R];
+#pragma unroll
+    for (int q = 0; q < n; ++q) {
+      float f[R];
+      Row<T>::values(v[q], f);
+      const int u = min((k0 + q) * C + me, x.end);
+      const uint32_t w = bits[u >> 5] >> (u & 31) & ((1u << R) - 1);
+#pragma unroll
+      for (int j = 0; j < R; ++j) z[q * R + j] = f[j];
+      if (__builtin_amdgcn_ballot_w64(w != 0)) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) z[q * R + j] = w >> j & 1 ? -INFINITY : f[j];
+      }
+    }
+    float m = z[0];
+#pragma unroll
+    for (int i = 1; i < n * R; ++i) m = fmaxf(m, z[i]);
+    const float up = fmaxf(ref, m * (float)(inv_temp * kLog2eD)), base = up == -INFINITY ? 0.f : up;
+    s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
+    ref = up;
+#pragma unroll
+    for (int i = 0; i < n * R; ++i) s += fast_exp2(fmaf(z[i], (float)(inv_temp * kLog2eD), -base));
+  };
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  // LDS's share by way of registers, two stripes ahead
+#pragma unroll
+  for (int k = 0; k < kHoldLds; ++k) {
+    const Bits v = fetch(NR + k);
+    held[k][threadIdx.x] = v.w;
+  }
+#pragma unroll
+  for (int k = 0; k < NR; k += 2) absorb(Two{}, b + k, k);
+  Bits v[2] = {fetch(NR + kHoldLds), fetch(NR + kHoldLds + 1)};
+#pragma unroll 1
+  for (int k = 0; k < kHoldLds; ++k) {
+    Bits h;
+    h.w = held[k][threadIdx.x];     // (its own writes)
+    absorb(One{}, &h, NR + k);
+  }
+  for (int k = NR + kHoldLds; k < stripes; k += 2) {
+    const Bits now[2] = {v[0], v[1]};
+    v[0] = fetch(k + 2);
+    v[1] = fetch(k + 3);
+    absorb(Two{}, now, k);
+  }
+  const bool rim_named = rim >= 0 && (bits[rim >> 5] >> (rim & 31) & 1);
+  if (rim >= 0 && !rim_named) {
+    const float up = fmaxf(ref, zr * (float)(inv_temp * kLog2eD)), base = up == -INFINITY ? 0.f : up;
+    s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
+    ref = up;
+    s += fast_exp2(fmaf(zr, (float)(inv_temp * kLog2eD), -base));
+  }
+  const float wm = wave_max(ref);
+  if (lane == 0) red_m[wave] = wm;
+  lds_barrier();
+  float M = red_m[0];
+#pragma unroll
+  for (int w = 1; w < kStepWaves; ++w) M = fmaxf(M, red_m[w]);
+  s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - M));
+  if (lane == 0) red_s[wave] = s;
+  lds_barrier();
+  if (threadIdx.x == 0) {
+    float S = 0.f;
+    for (int w = 0; w < kStepWaves; ++w) S += red_s[w];
+    sum = make_float2(M, S);
+  }
+  lds_barrier();
+  const RowSums r = row_sums<kStepWaves>(e, z, inv_temp, &sum, 1, red);
+  // the gradient from the rounded log-sum-exps, as the backward by itself has them
+  const float all = (float)r.all, rest = (float)r.rest;
+  if (threadIdx.x == 0) {
+    loss[row] = (float)r.loss;
+    lse[row] = all;
+    lse[rows + row] = rest;
+  }
+  const RowGrad grad(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, all, rest);
+  G *out = dz + row * ldd - x.shift;
+  const bool vec = runs_aligned<G, R>(out);
+  auto put = [&](const Bits &v, int k) __attribute__((always_inline)) {
+    const int u = k * C + me;
+    if (u < x.shift || u + R > x.end) return;
+    float g[R];
+    Row<T>::values(v, g);
+#pragma unroll
+    for (int j = 0; j < R; ++j) g[j] = grad.other(g[j]);
+    if (vec) {
+      store_run<G, R>(out + u, g);
+    } else {
+#pragma unroll
+      for (int j = 0; j < R; ++j) stf(out + u + j, g[j]);
+    }
+  };
+  int k = stripes - 1;
+  if (k >= NR + kHoldLds) {
+    Bits a = fetch(k), c2 = fetch(k - 1);
+    for (; k >= NR + kHoldLds; --k) {
+      const Bits now = a;
+      a = c2;
+      if (k - 2 >= NR + kHoldLds) c2 = fetch(k - 2);
+      put(now, k);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < NR; ++k) put(b[k], k);
+#pragma unroll 1
+  for (int k = 0; k < kHoldLds; ++k) {
+    Bits h;
+    h.w = held[k][threadIdx.x];
+    put(h, NR + k);
+  }
+  if (rim >= 0) stf(out + rim, grad.other(zr));
+  __syncthreads();    // the named ones over what the runs left there
+  if (e.v >= 0) stf(out + e.v + x.shift, grad.named(e, z, inv_temp, all));
 }
 
 // ------------------------------------------------------------------ host
@@ -902,6 +1086,19 @@ void launch_grad(const aj_logits &lg, const aj_teacher &t, const float *lse, voi
                                                        teacher_of(t), lg.inv_temp, lse, (float *)dz, ldd);
 }
 
+// One workgroup a row from this many rows (two rounds of the CUs) and values on.
+constexpr int kStepRows = 512, kStepLeast = 32768;
+template <typename T>
+void launch_step(const aj_logits &lg, const aj_teacher &t, float *loss, float *lse, int32_t *err, void *dz,
+                 int64_t ldd, int d_dtype, hipStream_t st) {
+  if (d_dtype == AJ_BF16)
+    distill_step_kernel<T, bf16_t><<<lg.rows, kStepNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, lg.rows, teacher_of(t),
+                                                                lg.inv_temp, loss, lse, err, (bf16_t *)dz, ldd);
+  else
+    distill_step_kernel<T, float><<<lg.rows, kStepNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, lg.rows, teacher_of(t),
+                                                               lg.inv_temp, loss, lse, err, (float *)dz, ldd);
+}
+
 size_t distill_ws(int rows, int vocab) {
   auto parts = [&](int width) { return (vocab + 7 + width - 1) / width; };
   aj::Carver cv(nullptr);
@@ -986,6 +1183,16 @@ extern "C" int aj_distill_loss_fwd_bwd(const aj_logits *lg, const aj_teacher *t,
   if ((r = check_logits(lg, name)) || (r = check_teacher(lg, t, name)) ||
       (r = check_grad(lg, dlogits, ldd, d_dtype, name)))
     return r;
+  if (lg->rows >= kStepRows && lg->vocab >= kStepLeast && lg->vocab <= kStepVocab) {
+    AJ_REQUIRE(loss && lse && ws, AJ_ERR_NULL, "%s: null pointer", name);
+    const size_t need = distill_ws(lg->rows, lg->vocab);
+    AJ_REQUIRE(ws_bytes >= need, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes, need);
+    hipStream_t st = (hipStream_t)stream;
+    if (lg->dtype == AJ_BF16) launch_step<bf16_t>(*lg, *t, loss, lse, err, dlogits, ldd, d_dtype, st);
+    else launch_step<float>(*lg, *t, loss, lse, err, dlogits, ldd, d_dtype, st);
+    if (stats) distill_stats_kernel<<<1, 1024, 0, st>>>(loss, t->weight, lg->rows, t->coef, stats);
+    return aj::check_launch(name);
+  }
   if ((r = aj_distill_loss_fwd(lg, t, loss, lse, stats, err, ws, ws_bytes, stream))) return r;
   return aj_distill_loss_bwd(lg, t, lse, dlogits, ldd, d_dtype, stream);
 }

@@ -224,6 +224,38 @@ def test_distill(rows, vocab, k, pad, offset, dtype, grad, tail):
         assert a == b if isinstance(a, int) else torch.equal(a, b)
 
 
+@pytest.mark.parametrize("tail", [False, True], ids=["listed", "tail"])
+@pytest.mark.parametrize("dtype, grad", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("vocab, k, pad, offset", [(32768, 20, 0, 0), (40001, 256, 3, 1), (100003, 7, 0, 2),
+                                                   (152064, 64, 0, 0)])
+def test_many_long_rows(vocab, k, pad, offset, dtype, grad, tail):
+    """Enough rows for a workgroup each: values kept on the chip, or read again, or both."""
+    rows = 515
+    z, view = make(rows, vocab, dtype, pad, seed=9, offset=offset)
+    some = torch.cat([torch.arange(4), torch.arange(rows - 3, rows)])
+    idx, lp = lists(z[some], k, 9, 1.0)
+    idx = idx[torch.arange(rows) % 4].clone()
+    lp = lp[torch.arange(rows) % 4].clone()
+    idx[some], lp[some] = lists(z[some], k, 9, 1.0)
+    w = torch.rand(rows, generator=torch.Generator().manual_seed(3)) + 0.5
+    got = distill(view, 1.0, idx, lp, tail, w, 1.0, grad)
+    want = definition(z[some], 1.0, idx[some], lp[some], tail, w[some].double())
+    check_distill((got[0][some], got[1][:, some], got[2][some], None, None), want, grad, 1.0)
+    apart = distill(view, 1.0, idx, lp, tail, w, 1.0, grad, part="apart")
+    assert bool(((got[0] - apart[0]).abs() <= 3 * LSE + 8 * E * (apart[1][0].abs() + apart[0].abs())).all())
+    u = 2.0 ** -7 if grad == "bf16" else 0.0
+    # each is off by its q's error, and a named token's gradient w (M q - p) may be far
+    # smaller than w q <= |gradient| + w p
+    p = lp.double().exp() if tail else torch.softmax(torch.where(idx >= 0, lp, -math.inf).double(), 1).nan_to_num()
+    at = torch.where(idx >= 0, idx, idx[:, :1].clamp(min=0)).long()
+    size = apart[2].double().abs()
+    size.scatter_add_(1, at, torch.where(idx >= 0, p, 0.0) * w[:, None].double() * 2)
+    off = (got[2].double() - apart[2].double()).abs()
+    assert bool((off <= u * apart[2].double().abs() + (2 * LSE + 300 * E) * size + 1e-37).all())
+    if dtype == grad:
+        assert torch.equal(distill(view, 1.0, idx, lp, tail, w, 1.0, grad, inplace=True)[2], got[2])
+
+
 @pytest.mark.parametrize("part", ["step", "apart"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gradient_in_the_logits_place(dtype, part):
