@@ -534,7 +534,7 @@ struct Listed {
   int v;          // -1: nothing
   double p;       // the teacher's probability (tail 0: renormalised over the list)
   double logp;
-  double mass, rest;   // of the whole row: sum of p and what is left of 1 (tail 1)
+  double mass, rest;   // of the whole row: sum of p, and of that what is left of 1 (tail 1)
 };
 
 template <int WAVES> AJ_DEV double block_sum(double v, double *red) {
@@ -592,39 +592,46 @@ AJ_DEV Listed listed(const Teacher &t, int64_t row, int vocab, int32_t *err, int
     const double ex = lp == -INFINITY ? 0.0 : exp(lp - m);
     const double s = block_sum<WAVES>(ex, red);
     e.p = s == 0.0 ? 0.0 : ex / s;
-    e.logp = lp - m - log(s);
+    e.logp = e.p == 0.0 ? -INFINITY : lp - m - log(s);   // (most waves hold no entry)
     e.mass = s == 0.0 ? 0.0 : 1.0;
     e.rest = 0.0;
   }
   return e;
 }
 
-// What a row's loss and gradient come from: log-sum-exps of the whole row and of the
-// values not named, and the loss.
-struct RowSums { double all, rest, loss; };
-// ms (parts of them): the others' sums as powers of two and factors; z: this thread's named value
+// Of a row's named values: their log-sum-exp and sum p (log p - z inv_temp).  (Known before
+// the others' sum is: what comes after that is on every row's critical path.)
+struct NamedSums { double list, term; };
 template <int WAVES>
-AJ_DEV RowSums row_sums(const Listed &e, double z, double inv_temp, const float2 *ms, int parts, double *red) {
-  RowSums r;
-  const double c = inv_temp * kLog2eD;
-  double M = -INFINITY;
-  for (int q = threadIdx.x; q < parts; q += 64 * WAVES) M = max(M, (double)ms[q].x);
-  M = block_max<WAVES>(M, red);
-  double s = 0.0;
-  for (int q = threadIdx.x; q < parts; q += 64 * WAVES)
-    s += ms[q].x == -INFINITY && ms[q].y == 0.f ? 0.0 : (double)ms[q].y * exp2((double)ms[q].x - M);
-  s = block_sum<WAVES>(s, red);
-  r.rest = log_of(M, s);
-  const double mz = block_max<WAVES>(z, red);
+AJ_DEV NamedSums named_sums(const Listed &e, double z, double inv_temp, double *red) {
+  const double c = inv_temp * kLog2eD, mz = block_max<WAVES>(z, red);
   const double sz = block_sum<WAVES>(z == -INFINITY ? 0.0 : exp2((z - mz) * c), red);
-  const double list = sz == 0.0 ? -INFINITY : (mz * c + log2(sz)) * kLn2D;
-  const double hi = max(r.rest, list);
-  r.all = r.rest + list;     // NaN where one is
-  if (r.all == r.all || hi == -INFINITY)
-    r.all = hi == -INFINITY ? -INFINITY : hi + log(exp(r.rest - hi) + exp(list - hi));
   double term = 0.0;
-  if (e.p > 0.0 || e.p != e.p) term = e.p * (e.logp - (z * inv_temp - r.all));
-  r.loss = block_sum<WAVES>(term, red);
+  if (e.p > 0.0 || e.p != e.p) term = e.p * (e.logp - z * inv_temp);
+  return {sz == 0.0 ? -INFINITY : (mz * c + log2(sz)) * kLn2D, block_sum<WAVES>(term, red)};
+}
+
+// A row's log-sum-exps, of all values and of those not named, and its loss; in one wave.
+// ms: the sums of the values not named, as powers of two and factors.
+struct RowSums { double all, rest, loss; };
+AJ_DEV RowSums row_sums(const Listed &e, const NamedSums &n, const float2 *ms, int parts) {
+  const int lane = threadIdx.x & 63;
+  RowSums r;
+  double M = -INFINITY;
+  for (int q = lane; q < parts; q += 64) M = max(M, (double)ms[q].x);
+  M = wave_max(M);
+  double s = 0.0;
+  for (int q = lane; q < parts; q += 64)
+    s += ms[q].x == -INFINITY && ms[q].y == 0.f ? 0.0 : (double)ms[q].y * exp2((double)ms[q].x - M);
+  s = wave_sum(s);
+  r.rest = log_of(M, s);
+  const double hi = max(r.rest, n.list);
+  r.all = r.rest + n.list;     // NaN where one is
+  if (r.all == r.all || hi == -INFINITY)
+    r.all = hi == -INFINITY ? -INFINITY : hi + log(exp(r.rest - hi) + exp(n.list - hi));
+  r.loss = n.term;
+  const double p = e.mass - e.rest;
+  if (p != 0.0) r.loss += p * r.all;
   if (e.rest > 0.0) r.loss += e.rest * (log(e.rest) - (r.rest - r.all));
   return r;
 }
@@ -632,35 +639,39 @@ AJ_DEV RowSums row_sums(const Listed &e, double z, double inv_temp, const float2
 // The gradient of the values not named, 2^(z c - ref) f, and of a named one.
 struct RowGrad {
   float c, ref, f;
-  double w;
-  AJ_DEV RowGrad(const Teacher &t, const Listed &e, double inv_temp, double weight, double all, double rest) {
+  int none;       // nothing listed: no loss, no gradient, whatever the logits
+  double w, all;
+  AJ_DEV void init(const Teacher &t, const Listed &e, double inv_temp, double weight, double all_, double rest) {
+    all = all_;
     w = (double)t.coef * inv_temp * weight;
     const double l = t.tail ? rest : all;
     ref = l == -INFINITY ? 0.f : (float)(l * kLog2eD);
     c = (float)(inv_temp * kLog2eD);
     f = (float)(t.tail ? w * (e.mass * exp(rest - all) - e.rest) : w * e.mass);
-    if (e.mass == 0.0) f = 0.f;
     none = e.mass == 0.0;
   }
-  bool none;      // nothing listed: no loss, no gradient, whatever the logits
   AJ_DEV float other(float z) const { return none ? 0.f : fast_exp2(fmaf(z, c, -ref)) * f; }
-  AJ_DEV float named(const Listed &e, double z, double inv_temp, double all) const {
+  AJ_DEV float named(const Listed &e, double z, double inv_temp) const {
     return none ? 0.f : (float)(w * (e.mass * exp(z * inv_temp - all) - e.p));
   }
 };
 
 // Stores a run's gradients at out + u (whole: the run lies in the row and out is aligned as
 // it is).
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 template <typename G, int R> AJ_DEV void store_run(G *out, const float (&g)[R]) {
   if constexpr (sizeof(G) == 4) {
 #pragma unroll
     for (int j = 0; j < R; j += 4)
-      *reinterpret_cast<float4 *>(out + j) = make_float4(g[j], g[j + 1], g[j + 2], g[j + 3]);
+      __builtin_nontemporal_store(f32x4_t{g[j], g[j + 1], g[j + 2], g[j + 3]}, reinterpret_cast<f32x4_t *>(out + j));
   } else if constexpr (R == 4) {
-    *reinterpret_cast<uint2 *>(out) = make_uint2(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]));
+    __builtin_nontemporal_store(u32x2_t{f2bf2(g[0], g[1]), f2bf2(g[2], g[3])}, reinterpret_cast<u32x2_t *>(out));
   } else {
-    *reinterpret_cast<uint4 *>(out) =
-        make_uint4(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]), f2bf2(g[4], g[5]), f2bf2(g[6], g[7]));
+    __builtin_nontemporal_store(
+        u32x4_t{f2bf2(g[0], g[1]), f2bf2(g[2], g[3]), f2bf2(g[4], g[5]), f2bf2(g[6], g[7])},
+        reinterpret_cast<u32x4_t *>(out));
   }
 }
 template <typename G, int R> AJ_DEV bool runs_aligned(const G *out) {
@@ -746,7 +757,9 @@ __global__ __launch_bounds__(kNT) void distill_row_kernel(const void *logits, in
   const int64_t row = blockIdx.x;
   const Listed e = listed<kWaves>(t, row, vocab, err, ids, red);
   const double z = e.v >= 0 ? (double)ldf((const T *)logits + row * ld + e.v) : -INFINITY;
-  const RowSums r = row_sums<kWaves>(e, z, inv_temp, ms + row * parts, parts, red);
+  const NamedSums n = named_sums<kWaves>(e, z, inv_temp, red);
+  if (threadIdx.x >= 64) return;
+  const RowSums r = row_sums(e, n, ms + row * parts, parts);
   if (threadIdx.x == 0) {
     loss[row] = (float)r.loss;
     lse[row] = (float)r.all;
@@ -790,10 +803,13 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
   fetch(u0);
   const Listed e = listed<kWaves>(t, row, vocab, nullptr, ids, red);
   const double all = lse[row], others = lse[rows + row];
-  const RowGrad grad(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, all, others);
+  __shared__ RowGrad shared_grad;
+  if (threadIdx.x == 0) shared_grad.init(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, all, others);
+  __syncthreads();
+  const RowGrad grad = shared_grad;
   // this part's named values, read before any is written (d logits may be the logits)
   const bool mine = e.v >= 0 && e.v + x.shift >= u0 && e.v + x.shift < u1;
-  const float named = mine ? grad.named(e, ldf((const T *)logits + row * ld + e.v), inv_temp, all) : 0.f;
+  const float named = mine ? grad.named(e, ldf((const T *)logits + row * ld + e.v), inv_temp) : 0.f;
   __syncthreads();
   G *out = dz + row * ldd - x.shift;
   // runs are stored whole where d logits is aligned as the runs are
@@ -842,8 +858,12 @@ __global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logit
   __shared__ uint32_t bits[kBitWords];
   __shared__ int ids[kMaxK];
   __shared__ double red[kStepWaves];
-  __shared__ float red_m[kStepWaves], red_s[kStepWaves];
-  __shared__ float2 sum;
+  __shared__ float2 sums[kStepWaves];
+  __shared__ RowGrad shared_grad;
+  // what a thread knows of the list waits here: its registers hold the row
+  __shared__ double list_p[kMaxK];
+  __shared__ Listed shared_list;
+  __shared__ NamedSums shared_named;
   const int64_t row = blockIdx.x;
   const Row<T> x(logits, row, ld, vocab);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, me = threadIdx.x * R;
@@ -856,10 +876,20 @@ __global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logit
   const int rim = threadIdx.x < 2 * R ? x.rim(threadIdx.x) : -1;
   const float zr = rim >= 0 ? ldf(x.aligned + rim) : -INFINITY;
   for (int i = threadIdx.x; i <= x.end / 32; i += kStepNT) bits[i] = 0;
-  const Listed e = listed<kStepWaves>(t, row, vocab, err, ids, red);
-  const double z = e.v >= 0 ? (double)ldf((const T *)logits + row * ld + e.v) : -INFINITY;
-  mark(bits, e.v, x.shift, vocab, 0, x.end);
-  lds_barrier();
+  int my_v;
+  float my_z;
+  {
+    const Listed e = listed<kStepWaves>(t, row, vocab, err, ids, red);
+    my_v = e.v;
+    my_z = e.v >= 0 ? ldf((const T *)logits + row * ld + e.v) : -INFINITY;
+    mark(bits, e.v, x.shift, vocab, 0, x.end);
+    const NamedSums n = named_sums<kStepWaves>(e, my_z, inv_temp, red);
+    if ((int)threadIdx.x < t.k) list_p[threadIdx.x] = e.p;
+    if (threadIdx.x == 0) {
+      shared_list = e;
+      shared_named = n;
+    }
+  }
   float ref = -INFINITY, s = 0.f;
   // adds the values of N runs, at stripes k0, k0 + 1 and so on, that are not named
   auto absorb = [&](auto N, const Bits *v, int k0) __attribute__((always_inline)) {
@@ -889,6 +919,14 @@ __global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logit
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;
+  auto absorb_two = [&](const Bits *v, int k) __attribute__((always_inline)) {
+    if constexpr (R == 4) {
+      absorb(Two{}, v, k);
+    } else {      // (16 values at a time want more registers than there are)
+      absorb(One{}, v, k);
+      absorb(One{}, v + 1, k + 1);
+    }
+  };
   // LDS's share by way of registers, two stripes ahead
 #pragma unroll
   for (int k = 0; k < kHoldLds; ++k) {
@@ -896,7 +934,7 @@ __global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logit
     held[k][threadIdx.x] = v.w;
   }
 #pragma unroll
-  for (int k = 0; k < NR; k += 2) absorb(Two{}, b + k, k);
+  for (int k = 0; k < NR; k += 2) absorb_two(b + k, k);
   Bits v[2] = {fetch(NR + kHoldLds), fetch(NR + kHoldLds + 1)};
 #pragma unroll 1
   for (int k = 0; k < kHoldLds; ++k) {
@@ -908,7 +946,7 @@ __global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logit
     const Bits now[2] = {v[0], v[1]};
     v[0] = fetch(k + 2);
     v[1] = fetch(k + 3);
-    absorb(Two{}, now, k);
+    absorb_two(now, k);
   }
   const bool rim_named = rim >= 0 && (bits[rim >> 5] >> (rim & 31) & 1);
   if (rim >= 0 && !rim_named) {
@@ -918,29 +956,23 @@ __global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logit
     s += fast_exp2(fmaf(zr, (float)(inv_temp * kLog2eD), -base));
   }
   const float wm = wave_max(ref);
-  if (lane == 0) red_m[wave] = wm;
+  s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - wm));
+  if (lane == 0) sums[wave] = make_float2(wm, s);
   lds_barrier();
-  float M = red_m[0];
-#pragma unroll
-  for (int w = 1; w < kStepWaves; ++w) M = fmaxf(M, red_m[w]);
-  s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - M));
-  if (lane == 0) red_s[wave] = s;
-  lds_barrier();
-  if (threadIdx.x == 0) {
-    float S = 0.f;
-    for (int w = 0; w < kStepWaves; ++w) S += red_s[w];
-    sum = make_float2(M, S);
+  if (wave == 0) {
+    const Listed e = shared_list;     // (of the first thread, whose mass and rest are the row's)
+    const RowSums r = row_sums(e, shared_named, sums, kStepWaves);
+    // the gradient from the rounded log-sum-exps, as the backward by itself has them
+    const float all = (float)r.all, rest = (float)r.rest;
+    if (lane == 0) {
+      shared_grad.init(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, all, rest);
+      loss[row] = (float)r.loss;
+      lse[row] = all;
+      lse[rows + row] = rest;
+    }
   }
   lds_barrier();
-  const RowSums r = row_sums<kStepWaves>(e, z, inv_temp, &sum, 1, red);
-  // the gradient from the rounded log-sum-exps, as the backward by itself has them
-  const float all = (float)r.all, rest = (float)r.rest;
-  if (threadIdx.x == 0) {
-    loss[row] = (float)r.loss;
-    lse[row] = all;
-    lse[rows + row] = rest;
-  }
-  const RowGrad grad(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, all, rest);
+  const RowGrad grad = shared_grad;
   G *out = dz + row * ldd - x.shift;
   const bool vec = runs_aligned<G, R>(out);
   auto put = [&](const Bits &v, int k) __attribute__((always_inline)) {
@@ -977,7 +1009,11 @@ __global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logit
   }
   if (rim >= 0) stf(out + rim, grad.other(zr));
   __syncthreads();    // the named ones over what the runs left there
-  if (e.v >= 0) stf(out + e.v + x.shift, grad.named(e, z, inv_temp, all));
+  if (my_v >= 0) {
+    Listed e = shared_list;
+    e.p = list_p[threadIdx.x];
+    stf(out + my_v + x.shift, grad.named(e, my_z, inv_temp));
+  }
 }
 
 // ------------------------------------------------------------------ host
