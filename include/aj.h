@@ -548,6 +548,29 @@ int aj_distill_loss_fwd_bwd(const aj_logits *lg, const aj_teacher *t, float *los
                             float *stats, int32_t *err, void *dlogits, int64_t ldd, int32_t d_dtype,
                             void *ws, size_t ws_bytes, void *stream);
 
+/* The same at the LM head: final norm and vocab projection of one pack's targets, as
+ * aj_logprob_pg_loss_fwd / _bwd have them (in->tok, old_logprob, adv, inv_n_mask,
+ * ref_logprob and kl_coef are not read; cfg->vocab_chunk, clip_eps and keep_logits
+ * neither), then the calls above on their float32 logits, 8192 targets at a time.
+ * Row i of every list, loss and weight belongs to targets[i].
+ *   _topk: the teacher's lists; forward only.
+ *   _distill: the student's loss and its whole backward: dh float32 [n_tok, d] WRITTEN
+ * (rows that feed no target become 0), d_final_norm [d] and d_w_vocab [vocab, d]
+ * accumulated, NULL where frozen.  loss [n_tgt]; stats as above, or NULL.
+ * err: AJ_DEVERR_OFFSETS for a target outside the pack, and the lists' errors.
+ * ws: aj_lm_head_workspace_bytes(cfg, n_tgt, k): the logits of a slab (4 bytes each; with
+ * bfloat16 2 more for d logits) and 134 MB at most for split reductions. */
+size_t aj_lm_head_workspace_bytes(const aj_loss_cfg *cfg, int32_t n_tgt, int32_t k);
+int aj_lm_head_topk(const aj_loss_cfg *cfg, const aj_loss_in *in, const void *h,
+                    const void *final_norm, const void *w_vocab, float inv_temp, int32_t k,
+                    int32_t *idx, float *logprob, float *lse, int32_t *err, void *ws,
+                    size_t ws_bytes, void *stream);
+int aj_lm_head_distill(const aj_loss_cfg *cfg, const aj_loss_in *in, const void *h,
+                       const void *final_norm, const void *w_vocab, float inv_temp,
+                       const aj_teacher *t, float *loss, float *stats, float *dh,
+                       float *d_final_norm, float *d_w_vocab, int32_t *err, void *ws,
+                       size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------------------ 4. around the update
  * GRPO advantages (Section 3: GRPO-style updates; groups of rollouts per
  * task, e.g. group size 8 in Section 5.3).  The episodes of group g are

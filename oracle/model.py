@@ -94,13 +94,23 @@ def kv_head(h, n_q, n_kv):
     return (h * n_kv) // n_q
 
 
-def attention_segment(q, k, v, scale):
+def visible(L, window=0, n_sink=0):
+    """[L, L] mask: which keys (columns) each query of a segment sees.  Causal; with a window the
+    last `window` keys, the query's own among them, and the first n_sink."""
+    i, j = np.arange(L)[:, None], np.arange(L)[None, :]
+    see = j <= i
+    if window:
+        see &= (i - j < window) | (j < n_sink)
+    return see
+
+
+def attention_segment(q, k, v, scale, window=0, n_sink=0):
     """Causal attention of one segment. q [L,Hq,hd], k/v [L,Hkv,hd] -> o [L,Hq,hd], lse [Hq,L]."""
     L, Hq, hd = q.shape
     Hkv = k.shape[1]
     o = np.zeros_like(q)
     lse = np.zeros((Hq, L))
-    causal = np.tril(np.ones((L, L), dtype=bool))
+    causal = visible(L, window, n_sink)
     for h in range(Hq):
         g = kv_head(h, Hq, Hkv)
         s = (q[:, h, :] @ k[:, g, :].T) * scale
@@ -113,13 +123,13 @@ def attention_segment(q, k, v, scale):
     return o, lse
 
 
-def attention_segment_bwd(q, k, v, o, lse, do, scale):
+def attention_segment_bwd(q, k, v, o, lse, do, scale, window=0, n_sink=0):
     L, Hq, hd = q.shape
     Hkv = k.shape[1]
     dq = np.zeros_like(q)
     dk = np.zeros_like(k)
     dv = np.zeros_like(v)
-    causal = np.tril(np.ones((L, L), dtype=bool))
+    causal = visible(L, window, n_sink)
     for h in range(Hq):
         g = kv_head(h, Hq, Hkv)
         s = (q[:, h, :] @ k[:, g, :].T) * scale
@@ -186,7 +196,8 @@ def block_forward(x, W, cu_seqlens, pos, m):
     for s in range(len(cu_seqlens) - 1):
         lo, hi = int(cu_seqlens[s]), int(cu_seqlens[s + 1])
         if hi > lo:
-            o[lo:hi], lse[:, lo:hi] = attention_segment(qr[lo:hi], kr[lo:hi], v[lo:hi], scale)
+            o[lo:hi], lse[:, lo:hi] = attention_segment(qr[lo:hi], kr[lo:hi], v[lo:hi], scale,
+                                                           m.window, m.n_sink)
     of = o.reshape(n, Hq * hd)
     x1 = x + of @ W["w_o"].T
     b, r2 = rmsnorm(x1, W["mlp_norm"], m.rms_eps)
@@ -225,7 +236,7 @@ def block_backward(dy, c, W, cu_seqlens, m):
         if hi > lo:
             dqr[lo:hi], dkr[lo:hi], dv[lo:hi] = attention_segment_bwd(
                 c["qr"][lo:hi], c["kr"][lo:hi], c["v"][lo:hi], c["o"][lo:hi],
-                c["lse"][:, lo:hi], do[lo:hi], c["scale"])
+                c["lse"][:, lo:hi], do[lo:hi], c["scale"], m.window, m.n_sink)
     dq = rope_bwd(dqr, c["cos"], c["sin"])
     dk = rope_bwd(dkr, c["cos"], c["sin"])
     dqkv = np.concatenate([dq.reshape(n, -1), dk.reshape(n, -1), dv.reshape(n, -1)], axis=1)
@@ -339,6 +350,73 @@ def actor_update(packed, W, m, n_mask=None, ref_logprob=None, kl_coef=0.0):
     return {"logprob": logprob, "loss": loss, "n_mask": n_mask, "grads": g, "dx": dx,
             "dy": dy, "y": y, "tgt": tgt, "lse": lse_t, "ratio": r, "term": term,
             "kl": kl}
+
+
+def distill_terms(z, idx, logprob, tail):
+    """KL(teacher || student) of rows of (tempered) logits z against a teacher's lists, and its
+    gradient with respect to z.  idx [n, k] (< 0: unused), logprob [n, k]; tail: the rest of the
+    vocabulary is one more class, else the listed probabilities are renormalised."""
+    z = np.asarray(z, np.float64)
+    zm = z.max(axis=1, keepdims=True)
+    q = np.exp(z - zm)
+    q /= q.sum(axis=1, keepdims=True)
+    loss, dz = np.zeros(len(z)), np.zeros_like(z)
+    for i in range(len(z)):
+        on = idx[i] >= 0
+        at, p = idx[i][on], np.exp(np.asarray(logprob[i][on], np.float64))
+        others = np.ones(z.shape[1], dtype=bool)
+        others[at] = False
+        rest = max(0.0, 1.0 - p.sum()) if tail else 0.0
+        if not tail:
+            if p.sum() == 0.0:
+                continue
+            p = p / p.sum()
+        # the teacher over the whole vocabulary: what it does not list shared as the student does
+        full = np.zeros(z.shape[1])
+        full[at] = p
+        if rest > 0.0:
+            full[others] = rest * q[i][others] / q[i][others].sum()
+            loss[i] += rest * (np.log(rest) - np.log(q[i][others].sum()))
+        pos = p > 0.0
+        loss[i] += np.sum(p[pos] * (np.log(p[pos]) - np.log(q[i][at][pos])))
+        dz[i] = full.sum() * q[i] - full
+    return loss, dz
+
+
+def masked_targets(packed):
+    """The targets with a loss, ascending."""
+    tgt = target_positions(packed.cu_seqlens, packed.n_tok)
+    return tgt[packed.mask[tgt] == 1]
+
+
+def target_logits(packed, W, m):
+    """Logits of every masked target (one row each), float64."""
+    W = f64_weights(W)
+    y, _ = stack_forward(W["emb"][packed.tok], W, packed.cu_seqlens, packed.pos, m)
+    hn, _ = rmsnorm(y, W["final_norm"], m.rms_eps)
+    return hn[masked_targets(packed) - 1] @ W["w_vocab"].T
+
+
+def distill_update(packed, W, m, idx, logprob, tail, inv_temp=1.0, weight=None):
+    """Forward + backward of the distillation loss, the weighted mean over the masked targets of
+    KL(teacher || softmax(logits * inv_temp)); lists and weights per masked target."""
+    W = f64_weights(W)
+    tgt = masked_targets(packed)
+    x = W["emb"][packed.tok]
+    y, c = stack_forward(x, W, packed.cu_seqlens, packed.pos, m)
+    hn, rf = rmsnorm(y, W["final_norm"], m.rms_eps)
+    h = hn[tgt - 1]
+    loss, dz = distill_terms((h @ W["w_vocab"].T) * inv_temp, idx, logprob, tail)
+    w = (np.ones(len(tgt)) if weight is None else np.asarray(weight, np.float64)) / max(len(tgt), 1)
+    dz *= (w * inv_temp)[:, None]
+    dhn = np.zeros_like(hn)
+    np.add.at(dhn, tgt - 1, dz @ W["w_vocab"])
+    dy, dgf = rmsnorm_bwd(dhn, y, rf, W["final_norm"])
+    dx, g = stack_backward(dy, c, W, packed.cu_seqlens, m)
+    g["final_norm"], g["w_vocab"] = dgf, dz.T @ h
+    g["emb"] = np.zeros_like(W["emb"])
+    np.add.at(g["emb"], packed.tok, dx)
+    return {"loss": float(np.sum(loss * w)), "per_target": loss, "grads": g}
 
 
 def lora_effective(W, lora, scale, m):

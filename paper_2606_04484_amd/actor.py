@@ -319,15 +319,81 @@ class ActorUpdate:
                                      G.get("final_norm"), G.get("w_vocab"), self.lws,
                                      row_base=t0, ref_logprob=ref, kl_coef=kl_coef,
                                      w_vocab_t=wvt)
-            if self.lora is None:
-                C.aj_stack_bwd(self.bcfg, self.layers, cu, pos, p["max_len"], x, self.ckpt,
-                               self.saved, dh, dh, self.layer_grads, self.bws, base=t0)
-                C.aj_embed_bwd(tok, dh, G["emb"], self.ews)
-            else:
-                C.aj_stack_lora_bwd(self.bcfg, self.layers, self.adapters, self.rank, self.scale,
-                                    cu, pos, p["max_len"], x, self.ckpt, self.saved, dh, dh,
-                                    self.layer_grads, self.bws, base=t0)
+            self._stack_bwd(cu, pos, p["max_len"], tok, x, dh, t0)
         return self.stats
+
+    def _stack_bwd(self, cu, pos, max_len, tok, x, dh, t0):
+        """From the gradient of the last block's output (dh) through the blocks and the embedding."""
+        if self.lora is None:
+            C.aj_stack_bwd(self.bcfg, self.layers, cu, pos, max_len, x, self.ckpt,
+                           self.saved, dh, dh, self.layer_grads, self.bws, base=t0)
+            C.aj_embed_bwd(tok, dh, self.G["emb"], self.ews)
+        else:
+            C.aj_stack_lora_bwd(self.bcfg, self.layers, self.adapters, self.rank, self.scale,
+                                cu, pos, max_len, x, self.ckpt, self.saved, dh, dh,
+                                self.layer_grads, self.bws, base=t0)
+
+    def _head_buffers(self, L, k):
+        """Workspace of the LM head's calls on rows of logits, for the largest pack of L."""
+        self._buffers(max((p["t1"] - p["t0"] for p in L.packs), default=0), 0)
+        n = max((p["r1"] - p["r0"] for p in L.packs), default=0)
+        need = C.aj_lm_head_workspace_bytes(self.lcfg, n, k)
+        if getattr(self, "hws", None) is None or self.hws.numel() < need:
+            self.hws = torch.empty(max(need, 1), dtype=torch.uint8, device=self.dev)
+
+    def teacher_topk(self, L, k, temperature=1.0):
+        """What a student learns from this policy on layout L: the k most probable tokens at
+        every target, (idx int32, logprob float32) [n_mask, k], under softmax(logits /
+        temperature).  Forward only."""
+        self._head_buffers(L, k)
+        self.refresh_transposed()
+        idx = torch.empty(L.n_mask, k, dtype=torch.int32, device=self.dev)
+        logprob = torch.empty(L.n_mask, k, dtype=torch.float32, device=self.dev)
+        lse = torch.empty(L.n_mask, dtype=torch.float32, device=self.dev)
+        for p in L.packs:
+            t0, t1, s0, s1, r0, r1 = p["t0"], p["t1"], p["s0"], p["s1"], p["r0"], p["r1"]
+            if r0 == r1:
+                continue
+            x, y = self.x[:t1 - t0], self.y[:t1 - t0]
+            C.aj_embed_fwd(L.tok[t0:t1], self.W["emb"], x, self.err)
+            self._stack_fwd(L.cu_seqlens[s0:s1 + 1], L.pos[t0:t1], p["max_len"], x, y, t0)
+            C.aj_lm_head_topk(self.lcfg, L.targets[r0:r1], y, self.W["final_norm"], self.W["w_vocab"],
+                              1.0 / temperature, idx[r0:r1], logprob[r0:r1], lse[r0:r1], self.hws,
+                              row_base=t0, w_vocab_t=self._w_vocab_t(), err=self.err)
+        return idx, logprob
+
+    def distill_step(self, L, idx, logprob, temperature=1.0, tail=True, weight=None, coef=None):
+        """Forward + backward of the distillation loss over every pack of L; gradients accumulate
+        into self.G.  idx, logprob: a teacher's lists for L's targets (teacher_topk of the teacher,
+        at the same temperature); tail: the rest of the vocabulary is one more class, else the
+        lists are renormalised; weight: optional float32 [n_mask]; coef: default 1 / n_mask.
+        Returns float32 [2]: the loss (sum of coef * weight * KL), targets."""
+        if tuple(idx.shape) != tuple(logprob.shape) or idx.shape[0] != L.n_mask:
+            raise C.AjError(f"distill_step: lists {tuple(idx.shape)}, {tuple(logprob.shape)} for "
+                            f"{L.n_mask} targets")
+        self._head_buffers(L, idx.shape[1])
+        if coef is None:
+            coef = 1.0 / L.n_mask if L.n_mask else 0.0
+        W, G = self.W, self.G
+        stats = torch.zeros(2, dtype=torch.float32, device=self.dev)
+        loss = torch.empty(max(L.n_mask, 1), dtype=torch.float32, device=self.dev)
+        self.refresh_transposed()
+        for p in L.packs:
+            t0, t1, s0, s1, r0, r1 = p["t0"], p["t1"], p["s0"], p["s1"], p["r0"], p["r1"]
+            if r0 == r1:          # no target, no gradient
+                continue
+            x, y, dh = self.x[:t1 - t0], self.y[:t1 - t0], self.dh[:t1 - t0]
+            tok, pos, cu = L.tok[t0:t1], L.pos[t0:t1], L.cu_seqlens[s0:s1 + 1]
+            C.aj_embed_fwd(tok, W["emb"], x, self.err)
+            self._stack_fwd(cu, pos, p["max_len"], x, y, t0)
+            t = C.teacher(idx[r0:r1], logprob[r0:r1], tail=tail, coef=coef,
+                          weight=None if weight is None else weight[r0:r1])
+            C.aj_lm_head_distill(self.lcfg, L.targets[r0:r1], y, W["final_norm"], W["w_vocab"],
+                                 1.0 / temperature, t, loss[r0:r1], dh, G.get("final_norm"),
+                                 G.get("w_vocab"), self.hws, row_base=t0, stats=stats,
+                                 w_vocab_t=self._w_vocab_t(), err=self.err)
+            self._stack_bwd(cu, pos, p["max_len"], tok, x, dh, t0)
+        return stats
 
     def _stack_fwd(self, cu, pos, max_len, x, y, t0):
         if self.lora is None:

@@ -176,6 +176,11 @@ EXPORTS = {
     "aj_distill_loss_bwd": (C.c_int, [C.POINTER(Logits), C.POINTER(Teacher), vp, vp, i64, i32, vp]),
     "aj_distill_loss_fwd_bwd": (C.c_int, [C.POINTER(Logits), C.POINTER(Teacher), vp, vp, vp, vp,
                                           vp, i64, i32, vp, sz, vp]),
+    "aj_lm_head_workspace_bytes": (sz, [C.POINTER(LossCfg), i32, i32]),
+    "aj_lm_head_topk": (C.c_int, [C.POINTER(LossCfg), C.POINTER(LossIn), vp, vp, vp, f32, i32, vp,
+                                  vp, vp, vp, vp, sz, vp]),
+    "aj_lm_head_distill": (C.c_int, [C.POINTER(LossCfg), C.POINTER(LossIn), vp, vp, vp, f32,
+                                     C.POINTER(Teacher), vp, vp, vp, vp, vp, vp, vp, sz, vp]),
     "aj_grpo_advantages": (C.c_int, [i32, vp, vp, f32, vp, vp, vp, vp]),
     "aj_select_workspace_bytes": (sz, [i32, i32]),
     "aj_select_episodes": (C.c_int, [C.POINTER(Timelines), vp, vp, C.POINTER(TimelinesOut), vp,
@@ -655,6 +660,54 @@ def aj_distill_loss_fwd_bwd(logits, inv_temp, t, loss, lse, dlogits, ws, stats=N
     _check(lib().aj_distill_loss_fwd_bwd(C.byref(lg), C.byref(t), ptr(loss), ptr(lse), ptr(stats),
                                          ptr(err), *_dlogits(name, logits, dlogits),
                                          *_workspace(name, ws), stream_handle(stream)), name)
+
+
+def aj_lm_head_workspace_bytes(cfg, n_tgt, k):
+    return int(lib().aj_lm_head_workspace_bytes(C.byref(cfg), int(n_tgt), int(k)))
+
+
+def _head(name, cfg, targets, h, final_norm, w_vocab, row_base, w_vocab_t):
+    dt = (torch.bfloat16 if cfg.dtype == AJ_BF16 else torch.float32,)
+    d, v = cfg.d_model, cfg.vocab
+    ops = {"targets": (targets, (torch.int32,), (targets.numel(),)), "h": (h, dt, (h.shape[0], d)),
+           "final_norm": (final_norm, dt, (d,)), "w_vocab": (w_vocab, dt, (v, d))}
+    if w_vocab_t is not None:
+        ops["w_vocab_t"] = (w_vocab_t, dt, (d, v))
+    _operands(name, ops)
+    return LossIn(h.shape[0], targets.numel(), row_base, ptr(targets), None, None, None, 0.0, None,
+                  0.0, ptr(w_vocab_t))
+
+
+def aj_lm_head_topk(cfg, targets, h, final_norm, w_vocab, inv_temp, idx, logprob, lse, ws,
+                    row_base=0, w_vocab_t=None, err=None, stream=None):
+    """aj_topk_logprob of the targets' logits: idx int32, logprob float32 [n_tgt, k], lse
+    float32 [n_tgt]; cfg: loss_cfg."""
+    name = "aj_lm_head_topk"
+    a = _head(name, cfg, targets, h, final_norm, w_vocab, row_base, w_vocab_t)
+    n, k = a.n_tgt, idx.shape[1]
+    _operands(name, {"idx": (idx, (torch.int32,), (n, k)), "logprob": (logprob, (torch.float32,), (n, k)),
+                     "lse": (lse, (torch.float32,), (n,))})
+    _check(lib().aj_lm_head_topk(C.byref(cfg), C.byref(a), ptr(h), ptr(final_norm), ptr(w_vocab), inv_temp, k,
+                                 ptr(idx), ptr(logprob), ptr(lse), ptr(err), *_workspace(name, ws),
+                                 stream_handle(stream)), name)
+
+
+def aj_lm_head_distill(cfg, targets, h, final_norm, w_vocab, inv_temp, t, loss, dh, d_final_norm,
+                       d_w_vocab, ws, row_base=0, w_vocab_t=None, stats=None, err=None, stream=None):
+    """The distillation loss of the targets and its backward into dh (written), d_final_norm
+    and d_w_vocab (accumulated; None: frozen); t: of teacher()."""
+    name = "aj_lm_head_distill"
+    a = _head(name, cfg, targets, h, final_norm, w_vocab, row_base, w_vocab_t)
+    f, n = (torch.float32,), a.n_tgt
+    idx, logprob, weight = t.tensors
+    ops = {"idx": (idx, (torch.int32,), (n, t.k)), "logprob": (logprob, f, (n, t.k)), "weight": (weight, f, (n,)),
+           "loss": (loss, f, (n,)), "dh": (dh, f, tuple(h.shape)), "d_final_norm": (d_final_norm, f, (cfg.d_model,)),
+           "d_w_vocab": (d_w_vocab, f, (cfg.vocab, cfg.d_model)), "stats": (stats, f, (2,))}
+    optional = ("weight", "d_final_norm", "d_w_vocab", "stats")
+    _operands(name, {k: v for k, v in ops.items() if v[0] is not None or k not in optional})
+    _check(lib().aj_lm_head_distill(C.byref(cfg), C.byref(a), ptr(h), ptr(final_norm), ptr(w_vocab), inv_temp,
+                                    C.byref(t), ptr(loss), ptr(stats), ptr(dh), ptr(d_final_norm), ptr(d_w_vocab),
+                                    ptr(err), *_workspace(name, ws), stream_handle(stream)), name)
 
 
 # ------------------------------------------------------------------ around the update

@@ -721,7 +721,188 @@ int loss_bwd(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, const vo
   return aj::check_launch("aj_logprob_pg_loss_bwd");
 }
 
+// ---------------------------------------------------------------- teacher and student heads
+// Slabs of this many targets' logits at a time: float32 [slab, vocab] (5 GB of a 152064
+// vocabulary), which the top k or the distillation loss read, and the slab's d logits beside
+// them; the d W product's reduction is as long as a slab, and every slab adds to all of d W.
+constexpr int kHeadSlab = 8192;
+
+struct HeadWs {
+  void *hn, *dz;
+  float *rstd, *z, *dhn, *dg_part, *splitk, *lse;
+  size_t splitk_floats, rows_ws_bytes, bytes;
+  char *rows_ws;
+  int32_t *tpos, *trow;
+};
+
+HeadWs carve_head(const aj_loss_cfg &c, int n_tgt, int k, void *base) {
+  const bool f32 = c.dtype != AJ_BF16;
+  const int slab = std::min(n_tgt, kHeadSlab);
+  aj::Carver cv(base);
+  HeadWs w;
+  w.hn = cv.take<char>((int64_t)n_tgt * c.d_model * (f32 ? 4 : 2));
+  w.rstd = cv.take<float>(n_tgt);
+  w.tpos = cv.take<int32_t>(n_tgt);
+  w.trow = cv.take<int32_t>(n_tgt);
+  w.z = cv.take<float>((int64_t)slab * c.vocab);
+  // float32: d logits over the logits
+  w.dz = f32 ? (void *)w.z : cv.take<char>((int64_t)slab * c.vocab * 2);
+  w.lse = cv.take<float>(2 * (int64_t)slab);
+  w.dhn = cv.take<float>((int64_t)n_tgt * c.d_model);
+  w.dg_part = cv.take<float>(aj::rmsnorm_bwd_part_floats(n_tgt, c.d_model));
+  w.splitk_floats = std::max(aj::gemm_partial_floats(c.vocab, c.d_model, f32),
+                             aj::gemm_partial_floats(slab, c.d_model, f32));
+  w.splitk = cv.take<float>(w.splitk_floats);
+  w.rows_ws_bytes = std::max(aj_topk_workspace_bytes(slab, c.vocab, k), aj_distill_workspace_bytes(slab, c.vocab, k));
+  w.rows_ws = cv.take<char>(w.rows_ws_bytes);
+  w.bytes = cv.bytes();
+  return w;
+}
+
+int check_head(const aj_loss_cfg *c, const aj_loss_in *in, int k, float inv_temp, const char *name) {
+  AJ_REQUIRE(c && in, AJ_ERR_NULL, "%s: null cfg/in", name);
+  AJ_REQUIRE(c->dtype == AJ_F32 || c->dtype == AJ_BF16, AJ_ERR_UNSUPPORTED, "%s: dtype", name);
+  AJ_REQUIRE(c->d_model > 0 && c->d_model % 8 == 0 && c->d_model <= 8192, AJ_ERR_SHAPE,
+             "%s: d_model %d", name, c->d_model);
+  AJ_REQUIRE(c->vocab > 0 && c->vocab <= 1 << 24, AJ_ERR_SHAPE, "%s: vocab %d (at most 2^24)", name, c->vocab);
+  AJ_REQUIRE(c->rms_eps > 0, AJ_ERR_SHAPE, "%s: eps", name);
+  AJ_REQUIRE(in->n_tok >= 0 && in->n_tgt >= 0 && in->n_tgt <= in->n_tok, AJ_ERR_SHAPE,
+             "%s: n_tok %d n_tgt %d", name, in->n_tok, in->n_tgt);
+  AJ_REQUIRE(!in->w_vocab_t || c->vocab % 8 == 0, AJ_ERR_SHAPE,
+             "%s: the transposed vocab weights need vocab %% 8 == 0 (vocab %d)", name, c->vocab);
+  AJ_REQUIRE(in->n_tgt == 0 || in->targets, AJ_ERR_NULL, "%s: null targets", name);
+  AJ_REQUIRE(k >= 1 && k <= 256, AJ_ERR_SHAPE, "%s: k %d (1..256)", name, k);
+  AJ_REQUIRE(inv_temp > 0.f && inv_temp <= 1e30f, AJ_ERR_SHAPE, "%s: inv_temp %g", name, (double)inv_temp);
+  return AJ_OK;
+}
+
+// The targets' normalised rows.
+template <typename T>
+void head_rows(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, const void *gf, const HeadWs &w,
+               int32_t *err, hipStream_t st) {
+  sanitize_targets_kernel<<<(in.n_tgt + 255) / 256, 256, 0, st>>>(in.n_tgt, in.targets, in.row_base, in.n_tok,
+                                                                  w.tpos, w.trow, err);
+  aj::rmsnorm_fwd<T>((const T *)h, (const T *)gf, in.n_tgt, c.d_model, c.rms_eps, w.trow, 0, (T *)w.hn, w.rstd, st);
+}
+
+// float32 logits of targets [r0, r0 + n)
+template <typename T>
+int head_logits(const aj_loss_cfg &c, const aj_loss_in &in, const void *w_vocab, const HeadWs &w, int r0, int n,
+                hipStream_t st) {
+  const bool t = sizeof(T) == 2 && in.w_vocab_t;
+  aj::Gemm g;
+  g.M = n; g.N = c.vocab; g.K = c.d_model;
+  g.A = (const T *)w.hn + (int64_t)r0 * c.d_model; g.lda = c.d_model;
+  g.B = t ? in.w_vocab_t : w_vocab; g.ldb = t ? c.vocab : c.d_model; g.b_kmajor = !t;
+  g.C = w.z; g.ldc = c.vocab; g.c_f32 = true;
+  return aj::gemm<T>(g, st);
+}
+
+template <typename T>
+int head_topk(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, const void *gf, const void *w_vocab,
+              float inv_temp, int k, int32_t *idx, float *logprob, float *lse, int32_t *err, const HeadWs &w,
+              hipStream_t st) {
+  head_rows<T>(c, in, h, gf, w, err, st);
+  for (int r0 = 0; r0 < in.n_tgt; r0 += kHeadSlab) {
+    const int n = std::min(kHeadSlab, in.n_tgt - r0);
+    int r;
+    if ((r = head_logits<T>(c, in, w_vocab, w, r0, n, st))) return r;
+    const aj_logits lg{n, c.vocab, c.vocab, AJ_F32, inv_temp, w.z};
+    if ((r = aj_topk_logprob(&lg, k, idx + (int64_t)r0 * k, logprob + (int64_t)r0 * k, lse + r0, w.rows_ws,
+                             w.rows_ws_bytes, st)))
+      return r;
+  }
+  return aj::check_launch("aj_lm_head_topk");
+}
+
+template <typename T>
+int head_distill(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, const void *gf, const void *w_vocab,
+                 float inv_temp, const aj_teacher &t, float *loss, float *stats, float *dh, float *dgf, float *dwv,
+                 int32_t *err, const HeadWs &w, hipStream_t st) {
+  const int d = c.d_model;
+  aj::fill_f32(dh, (int64_t)in.n_tok * d, 0.f, st);
+  if (in.n_tgt == 0) return aj::check_launch("aj_lm_head_distill");
+  head_rows<T>(c, in, h, gf, w, err, st);
+  aj::fill_f32(w.dhn, (int64_t)in.n_tgt * d, 0.f, st);
+  for (int r0 = 0; r0 < in.n_tgt; r0 += kHeadSlab) {
+    const int n = std::min(kHeadSlab, in.n_tgt - r0);
+    int r;
+    if ((r = head_logits<T>(c, in, w_vocab, w, r0, n, st))) return r;
+    const aj_logits lg{n, c.vocab, c.vocab, AJ_F32, inv_temp, w.z};
+    aj_teacher part = t;
+    part.idx += (int64_t)r0 * t.k;
+    part.logprob += (int64_t)r0 * t.k;
+    if (t.weight) part.weight += r0;
+    if ((r = aj_distill_loss_fwd_bwd(&lg, &part, loss + r0, w.lse, stats, err, w.dz, c.vocab, c.dtype, w.rows_ws,
+                                     w.rows_ws_bytes, st)))
+      return r;
+    aj::Gemm g;   // d hn = dz W
+    g.M = n; g.N = d; g.K = c.vocab; g.A = w.dz; g.lda = c.vocab;
+    g.B = w_vocab; g.ldb = d; g.b_kmajor = false;
+    g.C = w.dhn + (int64_t)r0 * d; g.ldc = d; g.out = aj::OUT_ACCUM_F32;
+    g.partial = w.splitk; g.partial_cap = w.splitk_floats;
+    if ((r = aj::gemm<T>(g, st))) return r;
+    if (!dwv) continue;   // frozen LM head
+    g = aj::Gemm();   // d W += dz^T hn
+    g.M = c.vocab; g.N = d; g.K = n; g.A = w.dz; g.lda = c.vocab; g.a_kmajor = false;
+    g.B = (const T *)w.hn + (int64_t)r0 * d; g.ldb = d; g.b_kmajor = false;
+    g.C = dwv; g.ldc = d; g.out = aj::OUT_ACCUM_F32;
+    g.partial = w.splitk; g.partial_cap = w.splitk_floats;
+    if ((r = aj::gemm<T>(g, st))) return r;
+  }
+  aj::rmsnorm_bwd<T>(w.dhn, (const T *)h, w.rstd, (const T *)gf, in.n_tgt, d, w.trow, 0, 1, nullptr, dh, nullptr,
+                     w.dg_part, dgf, st);
+  return aj::check_launch("aj_lm_head_distill");
+}
+
 }  // namespace
+
+extern "C" size_t aj_lm_head_workspace_bytes(const aj_loss_cfg *cfg, int32_t n_tgt, int32_t k) {
+  if (!cfg || n_tgt < 0 || k <= 0 || cfg->vocab <= 0 || cfg->d_model <= 0) return 0;
+  return carve_head(*cfg, n_tgt, k, nullptr).bytes;
+}
+
+extern "C" int aj_lm_head_topk(const aj_loss_cfg *cfg, const aj_loss_in *in, const void *h, const void *final_norm,
+                               const void *w_vocab, float inv_temp, int32_t k, int32_t *idx, float *logprob,
+                               float *lse, int32_t *err, void *ws, size_t ws_bytes, void *stream) {
+  const char *name = "aj_lm_head_topk";
+  int r;
+  if ((r = check_head(cfg, in, k, inv_temp, name))) return r;
+  AJ_REQUIRE(k <= cfg->vocab, AJ_ERR_SHAPE, "%s: k %d of vocab %d", name, k, cfg->vocab);
+  if (in->n_tgt == 0) return AJ_OK;
+  AJ_REQUIRE(h && final_norm && w_vocab && idx && logprob && lse && ws, AJ_ERR_NULL, "%s: null pointer", name);
+  const HeadWs w = carve_head(*cfg, in->n_tgt, k, ws);
+  AJ_REQUIRE(ws_bytes >= w.bytes, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes, w.bytes);
+  hipStream_t st = (hipStream_t)stream;
+  const aj::StageSpan span(st, AJ_KC_STAGE_LOSS);
+  if (cfg->dtype == AJ_BF16)
+    return head_topk<bf16_t>(*cfg, *in, h, final_norm, w_vocab, inv_temp, k, idx, logprob, lse, err, w, st);
+  return head_topk<float>(*cfg, *in, h, final_norm, w_vocab, inv_temp, k, idx, logprob, lse, err, w, st);
+}
+
+extern "C" int aj_lm_head_distill(const aj_loss_cfg *cfg, const aj_loss_in *in, const void *h,
+                                  const void *final_norm, const void *w_vocab, float inv_temp, const aj_teacher *t,
+                                  float *loss, float *stats, float *dh, float *d_final_norm, float *d_w_vocab,
+                                  int32_t *err, void *ws, size_t ws_bytes, void *stream) {
+  const char *name = "aj_lm_head_distill";
+  int r;
+  AJ_REQUIRE(t, AJ_ERR_NULL, "%s: null teacher", name);
+  if ((r = check_head(cfg, in, t->k, inv_temp, name))) return r;
+  if (in->n_tok == 0) return AJ_OK;
+  AJ_REQUIRE(dh, AJ_ERR_NULL, "%s: null dh", name);
+  AJ_REQUIRE(in->n_tgt == 0 || (h && final_norm && w_vocab && loss && ws && t->idx && t->logprob), AJ_ERR_NULL,
+             "%s: null pointer", name);
+  const HeadWs w = carve_head(*cfg, in->n_tgt, t->k, ws);
+  AJ_REQUIRE(in->n_tgt == 0 || ws_bytes >= w.bytes, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes,
+             w.bytes);
+  hipStream_t st = (hipStream_t)stream;
+  const aj::StageSpan span(st, AJ_KC_STAGE_LOSS);
+  if (cfg->dtype == AJ_BF16)
+    return head_distill<bf16_t>(*cfg, *in, h, final_norm, w_vocab, inv_temp, *t, loss, stats, dh, d_final_norm,
+                                d_w_vocab, err, w, st);
+  return head_distill<float>(*cfg, *in, h, final_norm, w_vocab, inv_temp, *t, loss, stats, dh, d_final_norm,
+                             d_w_vocab, err, w, st);
+}
 
 extern "C" size_t aj_loss_saved_bytes(const aj_loss_cfg *cfg, int32_t n_tgt) {
   if (!cfg || n_tgt < 0) return 0;

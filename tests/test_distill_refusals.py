@@ -101,3 +101,35 @@ def test_binding_looks_at_its_operands():
         capi.aj_distill_loss_fwd(z, 1.0, capi.teacher(idx, lp, weight=loss[:3]), loss, lse, ws)
     with pytest.raises(AjError, match="loss must be"):
         capi.aj_distill_loss_fwd(z, 1.0, t, None, lse, ws)
+
+
+def head(what, cfg=None, n_tok=10, n_tgt=4, targets=P, k=8, inv_temp=1.0, ws=BIG, w_t=None, dh=P, h=P):
+    L = capi.lib()
+    cfg = cfg or capi.LossCfg(64, 100, 128, 0.2, 1e-6, 1, 0)
+    a = capi.LossIn(n_tok, n_tgt, 0, targets, None, None, None, 0.0, None, 0.0, w_t)
+    if what == "topk":
+        return L.aj_lm_head_topk(C.byref(cfg), C.byref(a), h, P, P, inv_temp, k, P, P, P, None, P, ws, None)
+    return L.aj_lm_head_distill(C.byref(cfg), C.byref(a), h, P, P, inv_temp, C.byref(teach(k=k)), P, None, dh, P, P,
+                                None, P, ws, None)
+
+
+@pytest.mark.parametrize("what", ["topk", "distill"])
+def test_lm_head(what):
+    assert head(what, cfg=capi.LossCfg(60, 100, 128, 0.2, 1e-6, 1, 0)) == 2      # d_model % 8
+    assert head(what, cfg=capi.LossCfg(64, 0, 128, 0.2, 1e-6, 1, 0)) == 2
+    assert head(what, cfg=capi.LossCfg(64, 100, 128, 0.2, 0.0, 1, 0)) == 2
+    assert head(what, cfg=capi.LossCfg(64, 100, 128, 0.2, 1e-6, 2, 0)) == 3
+    assert head(what, n_tgt=11) == 2
+    assert head(what, n_tgt=-1) == 2
+    assert head(what, targets=None) == 1
+    assert head(what, k=0) == 2 and head(what, k=257) == 2
+    assert head(what, inv_temp=0.0) == 2 and head(what, inv_temp=float("nan")) == 2
+    assert head(what, w_t=P) == 2                                                # vocab % 8
+    assert head(what, h=None) == 1
+    assert head(what, ws=64) == 4
+    assert head(what, n_tok=0, n_tgt=0) == 0
+
+
+def test_lm_head_own():
+    assert head("topk", k=101) == 2          # more than the vocabulary
+    assert head("distill", dh=None) == 1
