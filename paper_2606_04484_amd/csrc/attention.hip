@@ -390,22 +390,44 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(WinAttnBwdArgs a) {
 // dK, dV rows of kv head g: sum over the query heads of the group and the
 // queries of the same segment at or after the key (with a window: the W of them
 // from the key on, all of them for a sink).
-template <typename T, int NC, bool WIN>
+enum { kCausal, kWindow, kFar };   // kFar: the far sinks, a chunk of one head's queries a workgroup
+
+template <typename T, int NC, int MODE>
 __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(WinAttnBwdArgs a) {
   __shared__ __attribute__((aligned(16))) float Qs[kStep<NC> * kLd<NC>], Ds[kStep<NC> * kLd<NC>];
   __shared__ __attribute__((aligned(16))) float Ls[kStep<NC>], Dl[kStep<NC>];
   const int hd = a.hd, ld = (a.Hq + 2 * a.Hkv) * hd;
-  const int g = blockIdx.y;
-  const int row0 = blockIdx.x * kRows;
+  const int group = a.Hq / a.Hkv;
+  const int g = MODE == kFar ? blockIdx.y / group : blockIdx.y;
+  // the query heads
+  const int h0 = MODE == kFar ? blockIdx.y : g * group, n_h = MODE == kFar ? 1 : group;
+  int row0 = blockIdx.x * kRows, q_lo = row0, s0 = 0, n_far = 0, slot = 0, q_hi = 0;
+  if constexpr (MODE == kFar) {
+    const int tiles = (a.n_sink + kRows - 1) / kRows;
+    slot = blockIdx.x / tiles;
+    const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, slot / 2 * kPlainSinkChunk + kPlainSinkChunk - 1);
+    s0 = a.cu_seqlens[seg] - a.base;
+    const int s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok), chunk = slot - s0 / kPlainSinkChunk * 2;
+    if (s0 < 0 || chunk < 0 || chunk * kPlainSinkChunk >= s1 - s0) return;
+    n_far = far_sinks(a, s1 - s0, kPlainSinkChunk);
+    row0 = s0 + blockIdx.x % tiles * kRows;
+    if (row0 - s0 >= n_far) return;
+    q_lo = s0 + chunk * kPlainSinkChunk;
+    q_hi = min(q_lo + kPlainSinkChunk, s1) - 1;
+  }
   const int lane = threadIdx.x & 63, w0 = row0 + 16 * (threadIdx.x >> 6);
   const int row = w0 + (lane & 15);           // the key row
-  const bool valid = row < a.n_tok;
+  const bool valid = MODE == kFar ? row < s0 + n_far : row < a.n_tok;
   const T *qkv = (const T *)a.qkv;
   const bool vec = vec4(a.qkv, ld, sizeof(T)), vecd = vec4(a.dout, (int64_t)a.Hq * hd, sizeof(T));
-  int end = valid ? seg_end(a, row) : 0;
-  int q_hi = seg_end(a, min(row0 + kRows, a.n_tok) - 1) - 1;
-  if constexpr (WIN) {
-    if (valid && row - seg_start(a, row) >= a.n_sink && end - row > a.window) end = row + a.window;
+  int end = MODE == kFar ? (valid ? q_hi + 1 : 0) : (valid ? seg_end(a, row) : 0);
+  if constexpr (MODE == kCausal) q_hi = seg_end(a, min(row0 + kRows, a.n_tok) - 1) - 1;
+  if constexpr (MODE == kWindow) {
+    if (valid && end - row > a.window) {
+      const int start = seg_start(a, row);
+      if (row - start >= a.n_sink) end = row + a.window;
+      else if (row - start < far_sinks(a, end - start, kPlainSinkChunk)) end = row;
+    }
     __shared__ int hi[4];     // the last query that any key of the workgroup meets
     int e = end;
 #pragma unroll
@@ -421,13 +443,12 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(WinAttnBwdArgs a) {
   f32x4_t k[NC], v[NC], dk[NC], dv[NC];
   own_row<T, NC>(k, qkv + (int64_t)row * ld + (a.Hq + g) * hd, hd, valid);
   own_row<T, NC>(v, qkv + (int64_t)row * ld + (a.Hq + a.Hkv + g) * hd, hd, valid);
-  const int group = a.Hq / a.Hkv;
-  // the steps over every query head of the group, in one sequence
-  const int n_q = q_hi >= row0 ? (q_hi - row0) / kStep<NC> + 1 : 0;
+  // the steps over every query head, in one sequence
+  const int n_q = q_hi >= q_lo ? (q_hi - q_lo) / kStep<NC> + 1 : 0;
   float4 qr[kFours<NC>], dr[kFours<NC>];
   float lr = 0.f, er = 0.f;
   auto fetch = [&](int i) {
-    const int h = g * group + i / n_q, q0 = row0 + i % n_q * kStep<NC>;
+    const int h = h0 + i / n_q, q0 = q_lo + i % n_q * kStep<NC>;
     fetch_rows<T, NC>(qr, qkv + h * hd, ld, hd, vec, q0, q_hi);
     fetch_rows<T, NC>(dr, (const T *)a.dout + h * hd, (int64_t)a.Hq * hd, hd, vecd, q0, q_hi);
     const int q = q0 + (int)threadIdx.x;
@@ -440,14 +461,14 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(WinAttnBwdArgs a) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) dk[c] = dv[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (n_q > 0) fetch(0);
-    for (int i = 0; i < group * n_q; ++i) {
-      const int q0 = row0 + i % n_q * kStep<NC>;
+    for (int i = 0; i < n_h * n_q; ++i) {
+      const int q0 = q_lo + i % n_q * kStep<NC>;
       __syncthreads();
       put_rows<NC>(Qs, qr);
       put_rows<NC>(Ds, dr);
       if ((int)threadIdx.x < kStep<NC>) Ls[threadIdx.x] = lr, Dl[threadIdx.x] = er;
       __syncthreads();
-      if (i + 1 < group * n_q) fetch(i + 1);
+      if (i + 1 < n_h * n_q) fetch(i + 1);
       for (int t = 0; t < kStep<NC> && q0 + t <= w_hi; t += 16) {
         if (q0 + t + 15 < w0) continue;
         const f32x4_t s = rows_dot<NC>(Qs + t * kLd<NC>, k);
@@ -471,9 +492,50 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(WinAttnBwdArgs a) {
   // not `||`: every thread takes both barriers
   if (any_nonfinite<NC>(dk, valid) | any_nonfinite<NC>(dv, valid)) walk(std::true_type{});
   if (!valid) return;
+  if constexpr (MODE == kFar) {
+    float *p = a.sink_part + (((int64_t)slot * a.Hq + h0) * a.n_sink + row - s0) * (2 * hd);
+    store_row<float, NC>(p, dk, hd, 1.f);
+    store_row<float, NC>(p + hd, dv, hd, 1.f);
+    return;
+  }
   T *base = (T *)a.dqkv + (int64_t)row * ld;
   store_row<T, NC>(base + (a.Hq + g) * hd, dk, hd, 1.f);
   store_row<T, NC>(base + (a.Hq + a.Hkv + g) * hd, dv, hd, 1.f);
+}
+
+// dK, dV of the far sinks: their chunks' and heads' sums, added up in their order (64 columns
+// of four features a workgroup, a quarter of the sums per wave).
+template <typename T>
+__global__ __launch_bounds__(256) void attn_far_sums_kernel(WinAttnBwdArgs a, int chunk, float scale) {
+  const int group = a.Hq / a.Hkv, w4 = a.hd / 2;   // 2 hd features of a key and KV head, in fours
+  const int per = (a.n_sink * a.Hkv * w4 + 63) / 64;
+  const int start = blockIdx.x / per;   // the segment that starts in this run of `chunk` rows
+  const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, start * chunk + chunk - 1);
+  const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
+  if (s0 < 0 || s0 / chunk != start) return;
+  const int n_far = far_sinks(a, s1 - s0, chunk);
+  if (n_far == 0) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int idx = blockIdx.x % per * 64 + lane;
+  const int col = idx % w4 * 4, g = idx / w4 % a.Hkv, j = idx / w4 / a.Hkv;
+  const int n = (s1 - s0 + chunk - 1) / chunk * group;   // (chunk, head of the group)
+  __shared__ f32x4_t red[4][64];
+  f32x4_t v{0.f, 0.f, 0.f, 0.f};
+  if (j < n_far) {
+    const float *p = a.sink_part + ((int64_t)2 * start * a.Hq * a.n_sink + j) * (2 * a.hd) + col;
+#pragma unroll 8
+    for (int i = w; i < n; i += 4)
+      v += *(const f32x4_t *)(p + ((int64_t)(i / group) * a.Hq + g * group + i % group) * a.n_sink * (2 * a.hd));
+  }
+  red[w][lane] = v;
+  __syncthreads();
+  if (w > 0 || j >= n_far) return;
+  v = red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane];
+  const bool is_k = col < a.hd;
+  T *out = (T *)a.dqkv + (int64_t)(s0 + j) * (a.Hq + 2 * a.Hkv) * a.hd + (a.Hq + (is_k ? g : a.Hkv + g)) * a.hd +
+           (is_k ? col : col - a.hd);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) stf(out + e, is_k ? v[e] * scale : v[e]);
 }
 
 // 16-feature chunks of a head, rounded up to an instantiated count
@@ -488,6 +550,19 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(WinAttnBwdArgs a) {
 }  // namespace
 
 bool windowed(int window, int n_tok) { return window > 0 && window < n_tok; }
+
+size_t attn_sink_floats(int window, int n_sink, int n_tok, int heads, int hd, int chunk) {
+  if (!windowed(window, n_tok) || n_sink == 0 || n_sink > kFarSinks || n_tok <= std::max(window, chunk)) return 0;
+  return (size_t)2 * (n_tok / chunk + 1) * heads * n_sink * 2 * hd;
+}
+
+template <typename T>
+void attn_far_sums(const WinAttnBwdArgs &a, int chunk, hipStream_t s) {
+  const unsigned blocks = (unsigned)(a.n_tok / chunk + 1) * ((a.n_sink * a.Hkv * (a.hd / 2) + 63) / 64);
+  // the matrix-core pass leaves dK unscaled
+  attn_far_sums_kernel<T><<<blocks, 256, 0, s>>>(a, chunk, chunk == kSinkChunk ? a.scale : 1.f);
+}
+template void attn_far_sums<bf16_t>(const WinAttnBwdArgs &, int, hipStream_t);
 
 template <typename T>
 int attn_fwd(const WinAttnArgs &args, hipStream_t s) {
@@ -526,10 +601,19 @@ int attn_bwd(const WinAttnBwdArgs &args, hipStream_t s) {
   const int blocks = (a.n_tok + kRows - 1) / kRows;
   if (win) {
     AJ_NC_DISPATCH(a.hd, (attn_dq_f32_kernel<T, NC, true><<<dim3(blocks, a.Hq), 256, 0, s>>>(a)));
-    AJ_NC_DISPATCH(a.hd, (attn_dkv_f32_kernel<T, NC, true><<<dim3(blocks, a.Hkv), 256, 0, s>>>(a)));
+    // (scratch of the matrix-core path's chunks holds none of these)
+    if (attn_sink_chunk(sizeof(T) == 4, a.hd) != kPlainSinkChunk ||
+        attn_sink_floats(a.window, a.n_sink, a.n_tok, a.Hq, a.hd, kPlainSinkChunk) == 0)
+      a.sink_part = nullptr;
+    AJ_NC_DISPATCH(a.hd, (attn_dkv_f32_kernel<T, NC, kWindow><<<dim3(blocks, a.Hkv), 256, 0, s>>>(a)));
+    if (a.sink_part) {
+      const dim3 far(2 * (a.n_tok / kPlainSinkChunk + 1) * ((a.n_sink + kRows - 1) / kRows), a.Hq);
+      AJ_NC_DISPATCH(a.hd, (attn_dkv_f32_kernel<T, NC, kFar><<<far, 256, 0, s>>>(a)));
+      attn_far_sums<T>(a, kPlainSinkChunk, s);
+    }
   } else {
     AJ_NC_DISPATCH(a.hd, (attn_dq_f32_kernel<T, NC, false><<<dim3(blocks, a.Hq), 256, 0, s>>>(a)));
-    AJ_NC_DISPATCH(a.hd, (attn_dkv_f32_kernel<T, NC, false><<<dim3(blocks, a.Hkv), 256, 0, s>>>(a)));
+    AJ_NC_DISPATCH(a.hd, (attn_dkv_f32_kernel<T, NC, kCausal><<<dim3(blocks, a.Hkv), 256, 0, s>>>(a)));
   }
   timing_end(s, tk);
   return check_launch("attention backward");
@@ -564,7 +648,8 @@ AttnWs carve_attn(const aj_attn_cfg &c, int n, void *base) {
   if (c.dtype == AJ_BF16)
     w.part_floats = std::min((size_t)2 * c.n_q_heads * n * c.head_dim, (size_t)64 << 20);
   w.part = cv.take<float>(w.part_floats);
-  w.sink = cv.take<float>(c.dtype == AJ_BF16 ? attn_sink_floats(c.window, c.n_sink, n, c.n_q_heads, c.head_dim) : 0);
+  w.sink = cv.take<float>(attn_sink_floats(c.window, c.n_sink, n, c.n_q_heads, c.head_dim,
+                                           attn_sink_chunk(c.dtype == AJ_F32, c.head_dim)));
   w.bytes = cv.bytes();
   return w;
 }

@@ -790,22 +790,6 @@ struct DkvSched {
   }
 };
 
-// The keys of a window pass: a key sees the W queries from itself on, and a sink all of
-// its segment's.  Left at that, the workgroup of a long segment's first keys would walk
-// every query of it while the others walk W: where that is a longer way than
-// kSinkChunk, the sinks that see past their window ("far") get no query in the window
-// pass and a pass of their own (attn_sinks_mfma_kernel), in chunks of kSinkChunk queries
-// of one head; a last kernel adds the chunks' float32 sums in order.  Chunk c of a
-// segment that starts at row s is number 2 floor(s / kSinkChunk) + c: such segments are
-// longer than kSinkChunk, so that their numbers never meet.
-constexpr int kSinkChunk = 1024;
-constexpr int kFarSinks = 128;     // most sinks that the far pass takes
-
-AJ_DEV int far_sinks(const WinAttnBwdArgs &a, int seg_len) {
-  if (a.sink_part == nullptr || seg_len <= max(a.window, kSinkChunk)) return 0;
-  return min(a.n_sink, seg_len - a.window);
-}
-
 template <int HD, int NW, bool WIN>
 __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a, int parts) {
   using TT = TokTile<HD, NW>;
@@ -836,7 +820,7 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
     if (kvv && ke - kv > a.window) {
       const int s0 = seg_start(a, kv);
       if (kv - s0 >= a.n_sink) ke = kv + a.window;
-      else if (kv - s0 < far_sinks(a, ke - s0)) ke = kv;
+      else if (kv - s0 < far_sinks(a, ke - s0, kSinkChunk)) ke = kv;
     }
   }
   const bf16_t *qkv = (const bf16_t *)a.qkv;
@@ -1187,7 +1171,7 @@ __global__ __launch_bounds__(256, 1) void attn_sinks_mfma_kernel(WinAttnBwdArgs 
   const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
   const int chunk = slot - s0 / kSinkChunk * 2;
   if (s0 < 0 || chunk < 0 || chunk * kSinkChunk >= s1 - s0) return;
-  const int n_far = far_sinks(a, s1 - s0);
+  const int n_far = far_sinks(a, s1 - s0, kSinkChunk);
   if (key0 >= n_far) return;
   const int qt0 = s0 + chunk * kSinkChunk, q_hi = min(qt0 + kSinkChunk, s1);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, hl = lane >> 5, lq = lane & 31;
@@ -1290,40 +1274,6 @@ __global__ __launch_bounds__(256, 1) void attn_sinks_mfma_kernel(WinAttnBwdArgs 
     const int key = key0 + e / (2 * HD), d = e % (2 * HD);
     *(f32x4_t *)(a.sink_part + (((int64_t)slot * a.Hq + h) * a.n_sink + key) * (2 * HD) + d) = v;
   }
-}
-
-// dK, dV of the far sinks: the sums of their chunks and heads, added up in their order
-// (64 columns of four features a workgroup, a quarter of the sums per wave).
-__global__ __launch_bounds__(256) void attn_far_sinks_kernel(WinAttnBwdArgs a) {
-  const int group = a.Hq / a.Hkv, w4 = a.hd / 2;   // 2 hd features of a key and KV head, in fours
-  const int per = (a.n_sink * a.Hkv * w4 + 63) / 64;
-  const int start = blockIdx.x / per;   // the segment that starts in this run of kSinkChunk rows
-  const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, start * kSinkChunk + kSinkChunk - 1);
-  const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
-  if (s0 < 0 || s0 / kSinkChunk != start) return;
-  const int n_far = far_sinks(a, s1 - s0);
-  if (n_far == 0) return;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int idx = blockIdx.x % per * 64 + lane;
-  const int col = idx % w4 * 4, g = idx / w4 % a.Hkv, j = idx / w4 / a.Hkv;
-  const int n = (s1 - s0 + kSinkChunk - 1) / kSinkChunk * group;   // (chunk, head of the group)
-  __shared__ f32x4_t red[4][64];
-  f32x4_t v{0.f, 0.f, 0.f, 0.f};
-  if (j < n_far) {
-    const float *p = a.sink_part + ((int64_t)2 * start * a.Hq * a.n_sink + j) * (2 * a.hd) + col;
-#pragma unroll 8
-    for (int i = w; i < n; i += 4)
-      v += *(const f32x4_t *)(p + ((int64_t)(i / group) * a.Hq + g * group + i % group) * a.n_sink * (2 * a.hd));
-  }
-  red[w][lane] = v;
-  __syncthreads();
-  if (w > 0 || j >= n_far) return;
-  v = red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane];
-  const bool is_k = col < a.hd;
-  if (is_k) v *= a.scale;
-  *(u32x2_t *)((bf16_t *)a.dqkv + (int64_t)(s0 + j) * (a.Hq + 2 * a.Hkv) * a.hd +
-               (a.Hq + (is_k ? g : a.Hkv + g)) * a.hd + (is_k ? col : col - a.hd)) =
-      u32x2_t{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
 
 __global__ __launch_bounds__(256) void attn_delta_bf16_kernel(WinAttnBwdArgs a) {
@@ -1445,11 +1395,6 @@ int attn_fwd_mfma(const WinAttnArgs &a, hipStream_t s) {
   return check_launch("attention forward (mfma)");
 }
 
-size_t attn_sink_floats(int window, int n_sink, int n_tok, int heads, int hd) {
-  if (!windowed(window, n_tok) || n_sink == 0 || n_sink > kFarSinks || n_tok <= std::max(window, kSinkChunk)) return 0;
-  return (size_t)2 * (n_tok / kSinkChunk + 1) * heads * n_sink * 2 * hd;
-}
-
 template <int HD>
 static void launch_bwd(const WinAttnBwdArgs &args, hipStream_t s) {
   WinAttnBwdArgs a = args;
@@ -1465,7 +1410,7 @@ static void launch_bwd(const WinAttnBwdArgs &args, hipStream_t s) {
   const int n_kt = (a.n_tok + 32 * kDkvWaves - 1) / (32 * kDkvWaves), parts = attn_dkv_parts(a);
   const unsigned grid = (unsigned)n_kt * a.Hkv * parts;
   const int starts = a.n_tok / kSinkChunk + 1;
-  if (!win || attn_sink_floats(a.window, a.n_sink, a.n_tok, a.Hq, HD) == 0) a.sink_part = nullptr;
+  if (!win || attn_sink_floats(a.window, a.n_sink, a.n_tok, a.Hq, HD, kSinkChunk) == 0) a.sink_part = nullptr;
   if (win) attn_dkv_mfma_kernel<HD, kDkvWaves, true><<<grid, 64 * kDkvWaves, 0, s>>>(a, parts);
   else attn_dkv_mfma_kernel<HD, kDkvWaves, false><<<grid, 64 * kDkvWaves, 0, s>>>(a, parts);
   const int key_tiles = (a.n_sink + 31) / 32;
@@ -1476,7 +1421,7 @@ static void launch_bwd(const WinAttnBwdArgs &args, hipStream_t s) {
     attn_dkv_parts_kernel<<<(unsigned)((n4 + 255) / 256), 256, 0, s>>>(a, parts);
   }
   if (a.sink_part)   // over the zeros that the window pass left there
-    attn_far_sinks_kernel<<<(unsigned)starts * ((a.n_sink * a.Hkv * (HD / 2) + 63) / 64), 256, 0, s>>>(a);
+    attn_far_sums<bf16_t>(a, kSinkChunk, s);
 }
 
 int attn_bwd_mfma(const WinAttnBwdArgs &a, hipStream_t s) {

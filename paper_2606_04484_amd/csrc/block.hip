@@ -79,7 +79,8 @@ BwdWs carve_bwd(const aj_block_cfg &c, int n, void *base) {
   w.splitk_floats = std::max(aj::gemm_partial_floats(2 * F, std::max(d, q), f32),
                              aj::gemm_partial_floats(n, 2 * F, f32));
   w.splitk = cv.take<float>(w.splitk_floats);
-  w.sink = cv.take<float>(f32 ? 0 : aj::attn_sink_floats(c.window, c.n_sink, n, c.n_q_heads, c.head_dim));
+  w.sink = cv.take<float>(aj::attn_sink_floats(c.window, c.n_sink, n, c.n_q_heads, c.head_dim,
+                                               aj::attn_sink_chunk(f32, c.head_dim)));
   w.bytes = cv.bytes();
   return w;
 }
@@ -357,10 +358,10 @@ int block_bwd(const aj_block_cfg &c, const aj_block_weights &w, const aj_varlen 
                                 sv.lse, ws.delta, ws.dqkv, 1.0f / sqrtf((float)hd)});
   ab.window = c.window;
   ab.n_sink = c.n_sink;
+  ab.sink_part = ws.sink;
   if constexpr (sizeof(T) == 2) {   // d gate / d up has been read: scratch
     ab.part = (float *)ws.dgu;
     ab.part_floats = (size_t)n * F;
-    ab.sink_part = ws.sink;
   }
   if ((r = attn_bwd<T>(ab, st))) return r;
   rope<T>((T *)ws.dqkv, n, v.pos, Hq + Hkv, qdim, hd, c.rope_theta, true, st);

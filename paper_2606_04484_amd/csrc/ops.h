@@ -152,9 +152,27 @@ bool windowed(int window, int n_tok);
 bool attn_mfma_supported(int hd, const void *p0, const void *p1, const void *p2);
 int attn_fwd_mfma(const WinAttnArgs &a, hipStream_t s);
 int attn_bwd_mfma(const WinAttnBwdArgs &a, hipStream_t s);
-// Floats of scratch that the windowed backward wants for the sums of sinks that see
-// queries past their window (0: none; it grows with n_tok).
-size_t attn_sink_floats(int window, int n_sink, int n_tok, int heads, int hd);
+// The dK/dV of a window pass gives every key the queries of its window, and a sink those of
+// its whole segment.  Left at that, the workgroup of a long segment's first keys walks every
+// query of it while the others walk a window: where that is a longer way than a chunk, the
+// sinks that see past their window ("far") get no query in the window pass and a pass of
+// their own, in chunks of queries of one head, whose float32 sums a last kernel adds in
+// order.  Chunk c of a segment that starts at row s is number 2 floor(s / chunk) + c: such
+// segments are longer than a chunk, so that their numbers never meet.  Sums of chunk
+// number x, head h: sink_part[x][h][sink][dK | dV].
+constexpr int kFarSinks = 128;     // most sinks that a far pass takes
+// queries in a chunk: of the matrix-core path (bfloat16, head_dim 64 or 128), of the plain one
+constexpr int kSinkChunk = 1024, kPlainSinkChunk = 256;
+inline int attn_sink_chunk(bool f32, int hd) { return !f32 && (hd == 64 || hd == 128) ? kSinkChunk : kPlainSinkChunk; }
+AJ_DEV int far_sinks(const WinAttnBwdArgs &a, int seg_len, int chunk) {
+  if (a.sink_part == nullptr || seg_len <= max(a.window, chunk)) return 0;
+  return min(a.n_sink, seg_len - a.window);
+}
+// Floats of scratch for these sums (0: no far pass; grows with n_tok).
+size_t attn_sink_floats(int window, int n_sink, int n_tok, int heads, int hd, int chunk);
+// dK, dV of the far sinks from their chunks' sums.
+template <typename T>
+void attn_far_sums(const WinAttnBwdArgs &a, int chunk, hipStream_t s);
 // its waves per workgroup in the forward and dQ passes, and the parts of a group's
 // query heads in the dK/dV pass
 int attn_row_waves(int n_tok, int n_seg, int heads);

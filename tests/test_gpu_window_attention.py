@@ -24,6 +24,8 @@ CASES = [
     ([1100], 2, 1, 64, 300, 130),            # sinks over more than 128 keys
     ([2500, 1, 1400], 2, 1, 128, 200, 4),
     ([2300], 7, 1, 64, 1024, 4),
+    ([40, 257, 600, 300, 1300], 4, 2, 32, 16, 128),    # (of 256 here)
+    ([258, 5, 700], 2, 1, 96, 1, 70),
     ([40, 1025, 1100, 30, 2049], 4, 2, 64, 16, 128),   # sinks whose queries are taken in chunks
     ([1030, 5, 1027], 2, 1, 128, 1, 40),
     ([3, 4100], 6, 2, 128, 1500, 33),
