@@ -133,6 +133,10 @@ AJ_DEV float order_value(uint32_t o) {
 }
 
 constexpr int kTopNT = 256, kTopWaves = kTopNT / 64;
+// Values a thread holds at a time.  32 would be 1.5 % faster on 4096 rows of 152064 float32 (448
+// against 456 us) but slower on 3000 of 151936 bfloat16 (264 against 224), whose rate is that
+// of the instructions: more of these waves fit a SIMD.
+constexpr int kTopValues = 16, kTopChunk = kTopNT * kTopValues;
 constexpr int kWaveHold = 5, kWaveCap = 64 * kWaveHold;    // candidates a wave keeps in LDS
 constexpr int kRankPad = 16;
 constexpr int kSlack = 64;       // over k that a last cut may leave to the ranking
@@ -277,7 +281,7 @@ AJ_DEV double log_of(double power, double sum) {
   return power == -INFINITY && sum == 0.0 ? -INFINITY : (power + log2(sum)) * kLn2D;
 }
 
-// One workgroup per part [u0, u0 + width) of a row, kTopNT * E values at a time, the next
+// One workgroup per part [u0, u0 + width) of a row, kTopChunk values at a time, the next
 // ones on their way meanwhile.  Gives the part's k largest places in order (0 after the
 // last), and its sum of 2^(z c) as a power of two (log2 units) and a factor.
 //
@@ -288,11 +292,11 @@ AJ_DEV double log_of(double power, double sum) {
 // of the list (or one a little lower), which is cut whenever twice k and more are in it, so
 // that of a long row few values pass.  Where too many pass all the same (equal values, NaN,
 // which is never below), a bisection over the places finds the k-th itself.
-template <typename T, int E>
-__global__ __launch_bounds__(kTopNT, E == 32 ? 4 : 5) void topk_part_kernel(
+template <typename T>
+__global__ __launch_bounds__(kTopNT, 5) void topk_part_kernel(
     const void *logits, int64_t ld, int vocab, int parts, int width, int k, float inv_temp, uint64_t *cand,
     float2 *ms, int32_t *idx, float *logprob, float *lse) {
-  constexpr int R = kRun<T>, Q = E / R, C = kTopNT * E;
+  constexpr int E = kTopValues, R = kRun<T>, Q = E / R, C = kTopNT * E;
   __shared__ __attribute__((aligned(16))) uint64_t lists[kTopWaves][kWaveCap + kRankPad];
   __shared__ uint64_t ranked[kMaxK];
   __shared__ float red_m[kTopWaves], red_s[kTopWaves];
@@ -1020,28 +1024,24 @@ __global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logit
 struct TopWs {
   uint64_t *cand;
   float2 *ms;
-  int parts, width, per_thread;
+  int parts, width;
   size_t bytes;
 };
 
-// Parts of a row: 4096 workgroups in all where the rows are fewer (four rounds of what
-// the card holds), in multiples of 32 values a thread; where even such parts are under
-// 512, parts of 16 a thread.  Never more than the join holds: candidates of all a row's
-// parts, kMaxCand.
+// Parts of a row: one where there are kTopRows rows and more, else about 4096 in all (three
+// rounds of what the card holds), but never more a row than the join holds: candidates of
+// all a row's parts, kMaxCand.
+constexpr int kTopRows = 1024;
 TopWs carve_top(int rows, int vocab, int k, void *base) {
   aj::Carver cv(base);
   TopWs w;
   const int64_t span = (int64_t)vocab + 7;   // a row may start 7 values past a run boundary
-  auto chunks = [&](int e) { return (span + kTopNT * e - 1) / (kTopNT * e); };
-  w.per_thread = rows * chunks(32) < 512 ? 16 : 32;
-  const int64_t n = chunks(w.per_thread);
-  int64_t parts = std::min(n, std::max<int64_t>(1, 4096 / std::max(rows, 1)));
-  parts = std::min<int64_t>(parts, kMaxCand / k);
-  w.width = (int)((n + parts - 1) / parts) * kTopNT * w.per_thread;
+  const int64_t n = (span + kTopChunk - 1) / kTopChunk;
+  const int64_t parts = rows >= kTopRows ? 1 : std::min({n, (int64_t)4096 / std::max(rows, 1), (int64_t)kMaxCand / k});
+  w.width = (int)((n + parts - 1) / parts) * kTopChunk;
   w.parts = (int)((span + w.width - 1) / w.width);
   // at least what fewer rows, cut finer, ask for
-  const size_t room =
-      (size_t)std::max((int64_t)rows * w.parts, std::min<int64_t>(rows * chunks(16), 4096));
+  const size_t room = (size_t)std::max((int64_t)rows * w.parts, std::min<int64_t>(rows * n, 4096));
   w.cand = cv.take<uint64_t>(room * k);
   w.ms = cv.take<float2>(room);
   w.bytes = cv.bytes();
@@ -1087,12 +1087,8 @@ template <typename T>
 void launch_topk(const aj_logits &lg, int k, int32_t *idx, float *logprob, float *lse, const TopWs &w,
                  hipStream_t st) {
   const unsigned grid = (unsigned)lg.rows * w.parts;
-  if (w.per_thread == 32)
-    topk_part_kernel<T, 32><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, lg.inv_temp,
-                                                     w.cand, w.ms, idx, logprob, lse);
-  else
-    topk_part_kernel<T, 16><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, lg.inv_temp,
-                                                     w.cand, w.ms, idx, logprob, lse);
+  topk_part_kernel<T><<<grid, kTopNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, w.width, k, lg.inv_temp, w.cand,
+                                               w.ms, idx, logprob, lse);
   if (w.parts > 1)
     topk_merge_kernel<T><<<lg.rows, kMergeNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, w.parts, k, lg.inv_temp,
                                                      w.cand, w.ms, idx, logprob, lse);
