@@ -330,28 +330,32 @@ def aj_embed_bwd(tok, dx, d_emb, ws, stream=None):
 # ------------------------------------------------------------------ attention
 
 def _operands(name, tensors):
-    """Checks {argument: (tensor, dtypes, shape)}: on the current GPU, of one of the dtypes, of
-    that shape, rows end to end."""
+    """Checks {argument: (tensor, dtypes, shape)}: of one of the dtypes, of that shape, rows end
+    to end, on the current GPU."""
     for arg, (t, dtypes, shape) in tensors.items():
-        if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or tuple(t.shape) != tuple(shape):
+        if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.shape != shape:
             got = f"{t.dtype} {tuple(t.shape)}" if isinstance(t, torch.Tensor) else type(t).__name__
             raise AjError(f"{name}: {arg} must be {' or '.join(str(d) for d in dtypes)} "
                           f"{tuple(shape)}, got {got}")
         if not t.is_contiguous():
             raise AjError(f"{name}: {arg} must be contiguous")
-    for arg, (t, _, _) in tensors.items():
-        _on_gpu(name, arg, t)
+    _on_gpu(name, **{arg: t for arg, (t, _, _) in tensors.items()})
 
 
-def _on_gpu(name, arg, t):
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise AjError(f"{name}: {arg} must be on the current GPU, is on {t.device}")
+def _on_gpu(name, **tensors):
+    here = None
+    for arg, t in tensors.items():
+        at = t.get_device()          # -1: host memory
+        if at >= 0 and here is None:
+            here = torch.cuda.current_device()
+        if at < 0 or at != here:
+            raise AjError(f"{name}: {arg} must be on the current GPU, is on {t.device}")
 
 
 def _workspace(name, ws):
     if not isinstance(ws, torch.Tensor) or not ws.is_contiguous():
         raise AjError(f"{name}: ws must be a contiguous tensor")
-    _on_gpu(name, "ws", ws)
+    _on_gpu(name, ws=ws)
     return ptr(ws), ws.numel() * ws.element_size()
 
 
@@ -596,7 +600,7 @@ def aj_topk_logprob(logits, inv_temp, idx, logprob, lse, ws, stream=None):
     _operands(name, {"idx": (idx, (torch.int32,), (lg.rows, k)),
                      "logprob": (logprob, (torch.float32,), (lg.rows, k)),
                      "lse": (lse, (torch.float32,), (lg.rows,))})
-    _on_gpu(name, "logits", logits)
+    _on_gpu(name, logits=logits)
     _check(lib().aj_topk_logprob(C.byref(lg), k, ptr(idx), ptr(logprob), ptr(lse),
                                  *_workspace(name, ws), stream_handle(stream)), name)
 
@@ -620,7 +624,7 @@ def _distill(name, logits, inv_temp, t, outs):
            "err": (outs.get("err"), (torch.int32,), (1,))}
     optional = {"weight", "stats", "err"} | ({"loss"} if "loss" not in outs else set())
     _operands(name, {k: v for k, v in ops.items() if v[0] is not None or k not in optional})
-    _on_gpu(name, "logits", logits)
+    _on_gpu(name, logits=logits)
     return lg
 
 
@@ -628,7 +632,7 @@ def _dlogits(name, logits, dlogits):
     rows, vocab, ld, dt = _rows_of(name, "dlogits", dlogits)
     if dlogits.shape != logits.shape:
         raise AjError(f"{name}: dlogits {tuple(dlogits.shape)} of logits {tuple(logits.shape)}")
-    _on_gpu(name, "dlogits", dlogits)
+    _on_gpu(name, dlogits=dlogits)
     return ptr(dlogits), ld, dt
 
 

@@ -849,17 +849,25 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
 // (kHoldLds), and forms the gradient from there; of a float32 row of 152064 values that
 // is 62 %, the rest is read again, newest first, while the caches still have it, and a
 // bfloat16 row of that length is kept whole.
-constexpr int kStepNT = 1024, kStepWaves = kStepNT / 64;
-constexpr int kHoldReg = 12, kHoldLds = 7, kBitWords = 8192;    // 16 KB a run; 32 KB of bits
-constexpr int kStepVocab = kBitWords * 32 - 16;
-template <typename T, typename G>
-__global__ __launch_bounds__(kStepNT) void distill_step_kernel(const void *logits, int64_t ld, int vocab,
-                                                               int rows, Teacher t, double inv_temp,
-                                                               float *loss, float *lse, int32_t *err, G *dz,
-                                                               int64_t ldd) {
-  constexpr int R = kRun<T>, C = kStepNT * R, NR = sizeof(T) == 4 ? kHoldReg : 8;
-  __shared__ __attribute__((aligned(16))) uint4 held[kHoldLds][kStepNT];
-  __shared__ uint32_t bits[kBitWords];
+// Rows of up to kSmallVocab values take four waves each, which hold all of a row in registers.
+struct LongRows {
+  static constexpr int NT = 1024, REG = 12, REG16 = 8, LDS = 8, WORDS = 6144;    // 128 KB of runs, 24 KB of bits
+};
+struct ShortRows {
+  static constexpr int NT = 256, REG = 12, REG16 = 8, LDS = 0, WORDS = 512;
+};
+constexpr int kStepVocab = LongRows::WORDS * 32 - 16;
+constexpr int kSmallVocab = ShortRows::NT * ShortRows::REG * 4 - 8;
+static_assert(kSmallVocab <= ShortRows::WORDS * 32 - 16 && kSmallVocab <= ShortRows::NT * ShortRows::REG16 * 8 - 8,
+              "short rows fit");
+template <typename T, typename G, typename S>
+__global__ __launch_bounds__(S::NT) void distill_step_kernel(const void *logits, int64_t ld, int vocab, int rows,
+                                                             Teacher t, double inv_temp, float *loss, float *lse,
+                                                             int32_t *err, G *dz, int64_t ldd) {
+  constexpr int kStepNT = S::NT, kStepWaves = kStepNT / 64, kHoldLds = S::LDS;
+  constexpr int R = kRun<T>, C = kStepNT * R, NR = sizeof(T) == 4 ? S::REG : S::REG16;
+  __shared__ __attribute__((aligned(16))) uint4 held[kHoldLds ? kHoldLds : 1][kStepNT];
+  __shared__ uint32_t bits[S::WORDS];
   __shared__ int ids[kMaxK];
   __shared__ double red[kStepWaves];
   __shared__ float2 sums[kStepWaves];
@@ -1118,17 +1126,21 @@ void launch_grad(const aj_logits &lg, const aj_teacher &t, const float *lse, voi
                                                        teacher_of(t), lg.inv_temp, lse, (float *)dz, ldd);
 }
 
-// One workgroup a row from this many rows (two rounds of the CUs) and values on.
+// Long rows take a workgroup each from this many rows (two rounds of the CUs) and values on; fewer
+// are cut into parts.
 constexpr int kStepRows = 512, kStepLeast = 32768;
-template <typename T>
+bool one_step(const aj_logits &lg) {
+  return lg.vocab <= kSmallVocab || (lg.rows >= kStepRows && lg.vocab >= kStepLeast && lg.vocab <= kStepVocab);
+}
+template <typename T, typename G>
 void launch_step(const aj_logits &lg, const aj_teacher &t, float *loss, float *lse, int32_t *err, void *dz,
-                 int64_t ldd, int d_dtype, hipStream_t st) {
-  if (d_dtype == AJ_BF16)
-    distill_step_kernel<T, bf16_t><<<lg.rows, kStepNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, lg.rows, teacher_of(t),
-                                                                lg.inv_temp, loss, lse, err, (bf16_t *)dz, ldd);
+                 int64_t ldd, hipStream_t st) {
+  if (lg.vocab <= kSmallVocab)
+    distill_step_kernel<T, G, ShortRows><<<lg.rows, ShortRows::NT, 0, st>>>(
+        lg.logits, lg.ld, lg.vocab, lg.rows, teacher_of(t), lg.inv_temp, loss, lse, err, (G *)dz, ldd);
   else
-    distill_step_kernel<T, float><<<lg.rows, kStepNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, lg.rows, teacher_of(t),
-                                                               lg.inv_temp, loss, lse, err, (float *)dz, ldd);
+    distill_step_kernel<T, G, LongRows><<<lg.rows, LongRows::NT, 0, st>>>(
+        lg.logits, lg.ld, lg.vocab, lg.rows, teacher_of(t), lg.inv_temp, loss, lse, err, (G *)dz, ldd);
 }
 
 size_t distill_ws(int rows, int vocab) {
@@ -1215,13 +1227,18 @@ extern "C" int aj_distill_loss_fwd_bwd(const aj_logits *lg, const aj_teacher *t,
   if ((r = check_logits(lg, name)) || (r = check_teacher(lg, t, name)) ||
       (r = check_grad(lg, dlogits, ldd, d_dtype, name)))
     return r;
-  if (lg->rows >= kStepRows && lg->vocab >= kStepLeast && lg->vocab <= kStepVocab) {
+  if (lg->rows > 0 && one_step(*lg)) {
     AJ_REQUIRE(loss && lse && ws, AJ_ERR_NULL, "%s: null pointer", name);
     const size_t need = distill_ws(lg->rows, lg->vocab);
     AJ_REQUIRE(ws_bytes >= need, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes, need);
     hipStream_t st = (hipStream_t)stream;
-    if (lg->dtype == AJ_BF16) launch_step<bf16_t>(*lg, *t, loss, lse, err, dlogits, ldd, d_dtype, st);
-    else launch_step<float>(*lg, *t, loss, lse, err, dlogits, ldd, d_dtype, st);
+    if (lg->dtype == AJ_BF16) {
+      if (d_dtype == AJ_BF16) launch_step<bf16_t, bf16_t>(*lg, *t, loss, lse, err, dlogits, ldd, st);
+      else launch_step<bf16_t, float>(*lg, *t, loss, lse, err, dlogits, ldd, st);
+    } else {
+      if (d_dtype == AJ_BF16) launch_step<float, bf16_t>(*lg, *t, loss, lse, err, dlogits, ldd, st);
+      else launch_step<float, float>(*lg, *t, loss, lse, err, dlogits, ldd, st);
+    }
     if (stats) distill_stats_kernel<<<1, 1024, 0, st>>>(loss, t->weight, lg->rows, t->coef, stats);
     return aj::check_launch(name);
   }

@@ -220,8 +220,12 @@ def test_distill(rows, vocab, k, pad, offset, dtype, grad, tail):
     assert got[3][0].item() == total or abs(got[3][0].item() - 1 - total) <= rows * 3 * LSE + 4 * E * (1 + abs(total)) * 2
     assert got[3][1].item() == 1 + rows
     apart = distill(view, inv, idx, lp, tail, w, coef, grad, part="apart")
-    for a, b in zip(got, apart):
-        assert a == b if isinstance(a, int) else torch.equal(a, b)
+    check_distill(apart, want, grad, inv)
+    again = distill(view, inv, idx, lp, tail, w, coef, grad)
+    for a, b, c in zip(got, apart, again):
+        assert a == c if isinstance(a, int) else torch.equal(a, c)
+        if vocab > 12280:     # few long rows: the same kernels (short ones sum in another order)
+            assert a == b if isinstance(a, int) else torch.equal(a, b)
 
 
 @pytest.mark.parametrize("tail", [False, True], ids=["listed", "tail"])
@@ -262,7 +266,7 @@ def test_gradient_in_the_logits_place(dtype, part):
     """d logits over the logits, whose rows lie apart: what is between them stays."""
     z, view = make(5, 9001, dtype, 7, seed=2, offset=3)
     idx, lp = lists(z, 50, 2, 1.0)
-    want = distill(view, 1.0, idx, lp, True, None, 1.0, dtype, part=part)
+    want = distill(view, 1.0, idx, lp, True, None, 1.0, dtype, part=part)   # (the same calls)
     got = distill(view, 1.0, idx, lp, True, None, 1.0, dtype, part=part, inplace=True)
     assert torch.equal(got[2], want[2]) and torch.equal(got[0], want[0])
     rest = torch.as_strided(view, (4, 7), (9008, 1), view.storage_offset() + 9001)
