@@ -29,6 +29,9 @@ CASES = [
     ([40, 1025, 1100, 30, 2049], 4, 2, 64, 16, 128),   # sinks whose queries are taken in chunks
     ([1030, 5, 1027], 2, 1, 128, 1, 40),
     ([3, 4100], 6, 2, 128, 1500, 33),
+    ([0, 130, 0, 0, 67, 0], 4, 2, 64, 20, 3),          # segments of no tokens
+    ([0, 1300, 0, 0, 1100, 0], 2, 1, 128, 200, 6),
+    ([0, 300, 0, 260, 0], 2, 1, 32, 30, 6),
     ([50, 60], 4, 2, 64, 4096, 4),           # a window that no row reaches past
 ]
 

@@ -36,6 +36,8 @@ def reference(qkv, lens, hq, hkv, hd, window, n_sink, dout=None, scale=None, bf1
     de = [new(*t.shape) for t in (q, k, v)]
     a = 0
     for L in lens:
+        if L == 0:
+            continue
         r = slice(a, a + L)
         see = visible(L, window, n_sink)
         for h in range(hq):
