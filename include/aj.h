@@ -245,7 +245,8 @@ typedef struct {
  * ws: at least aj_attention_workspace_bytes(cfg, n_tok), for either direction; it
  * carries nothing from one to the other.
  * Errors as the block's; n_tok at most 2^30, n_tok * n_q_heads below 2^32.  Infinities and
- * NaN as in the block.
+ * NaN in a row, or in its d out, reach with a window only what depends on that row by the
+ * formulas; without one as in the block.
  */
 typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim;
@@ -324,8 +325,8 @@ size_t aj_block_workspace_bytes(const aj_block_cfg *cfg, int32_t n_tok, int32_t 
  * that do not group evenly over the key/value heads, AJ_ERR_UNSUPPORTED for
  * a head_dim outside 8..128 (multiple of 8) or another dtype,
  * AJ_ERR_WORKSPACE for a short workspace.
- * Infinities and NaN in a row reach the rows that attend to it; with bfloat16
- * and head_dim 64 or 128 also other rows within the same tiles (64 keys, up to
+ * Infinities and NaN in a row reach the rows that attend to it; with bfloat16,
+ * head_dim 64 or 128 and no window also other rows within the same tiles (64 keys, up to
  * 256 queries), whose masked weights are zeros in the same matrix products. */
 int aj_varlen_block_fwd(const aj_block_cfg *cfg, const aj_block_weights *w, const aj_varlen *vl,
                         const void *x, void *y, void *saved, void *ws, size_t ws_bytes,

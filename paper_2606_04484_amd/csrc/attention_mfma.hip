@@ -414,6 +414,65 @@ AJ_DEV void cols_times_half(f32x16_t (&acc)[HD / 32], const TileLanes<HD> &L, co
   }
 }
 
+// ------------------------------------------------------------------ bad rows
+// A masked pair has weight 0 in the matrix products, and 0 times an infinity or a NaN is
+// a NaN.  With a window, a wave whose sums are not all finite takes its rows again, a pair
+// at a time and only those that are seen, so that a bad row stays with the rows that
+// attend to it (rows of padding, say, that nothing has written).  Finite rows pay one
+// check at the end.
+template <int N> AJ_DEV bool nonfinite(const f32x16_t (&v)[N]) {
+  float z = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = fmaf(v[i][r], 0.f, z);
+  return !(z == 0.f);
+}
+// This lane's half of the product of a row in memory (at its first feature) with the lane's
+// operand, the halves added up.  (hl, the lane's half, comes through a copy that the
+// compiler does not see into: else it forms addresses ahead of the main loops, which want
+// the registers.)
+AJ_DEV int opaque(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+template <int HD> AJ_DEV float row_dot(const bf16_t *row, const bf16x8_t (&b)[HD / 16], const int hl) {
+  float s = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < HD / 16; ++kk) {
+    const u32x4_t x = *(const u32x4_t *)(row + 16 * kk + 8 * hl);
+    const u32x4_t y = __builtin_bit_cast(u32x4_t, b[kk]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s);
+      s = fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), s);
+    }
+    __builtin_amdgcn_sched_barrier(0);   // no registers for more loads ahead
+  }
+  return s + __shfl_xor(s, 32, 64);
+}
+// acc (this lane's features) += w row, where `in`
+template <int HD> AJ_DEV void row_add(f32x16_t (&acc)[HD / 32], const bf16_t *row, float w, bool in, const int hl) {
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const u32x2_t x = *(const u32x2_t *)(row + 32 * i + 8 * r4 + 4 * hl);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+        acc[i][4 * r4 + e] = in ? fmaf(w, v, acc[i][4 * r4 + e]) : acc[i][4 * r4 + e];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+}
+template <int N> AJ_DEV void clear(f32x16_t (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[i][r] = 0.f;
+}
+
 // ------------------------------------------------------------------ forward
 // One workgroup: 32 * NW queries of one head (NW waves of 32), key tiles of 64
 // double-buffered and shared by all the waves; a lane owns one query.
@@ -536,6 +595,22 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_mfma_kernel(WinAttnArgs a
     if (it + 1 < kt.n) tile(it + 1, 1);
   }
   lsum += __shfl_xor(lsum, 32, 64);
+  if constexpr (WIN) {
+    if (__builtin_amdgcn_ballot_w64(qv && nonfinite(o))) {
+      const int half = opaque(hl);
+      clear(o);
+#pragma unroll 1
+      for (int it = 0; it < kt.n; ++it) {
+        const int k0 = kt.first(it), k1 = min(k0 + kTR, kt.rows(it));
+        const Seen seen(kt, it, k0, q, qs, low, a.n_sink, hl);
+#pragma unroll 1
+        for (int k = k0; k < k1; ++k) {
+          const float p = fast_exp2(fmaf(row_dot<HD>(kbase + (int64_t)k * ld, qf, half), c, -m));
+          row_add<HD>(o, vbase + (int64_t)k * ld, p, qv & seen.template has<WIN>(k - k0 - 4 * hl), half);
+        }
+      }
+    }
+  }
   if (!qv) return;
   const float inv = 1.f / lsum;
   bf16_t *out = (bf16_t *)a.o + (int64_t)q * a.Hq * HD + h * HD;
@@ -690,8 +765,38 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(WinAttnBwdArgs
     tile(it, 0);
     if (it + 1 < kt.n) tile(it + 1, 1);
   }
+  if constexpr (WIN) {
+    if (__builtin_amdgcn_ballot_w64(qv && nonfinite(acc))) {
+      // the operands are read again: kept for here, they would spill
+      const int half = opaque(hl), qr = min(opaque(q), a.n_tok - 1);
+      const bf16_t *qrow = qkv + (int64_t)qr * ld + h * HD, *drow = dout + (int64_t)qr * a.Hq * HD + h * HD;
+      const float lse = a.lse[(int64_t)h * a.n_tok + qr];
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        qf[kk] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(qrow + 16 * kk + 8 * half));
+        df[kk] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(drow + 16 * kk + 8 * half));
+      }
+      clear(acc);
+      KeyTiles<WIN> kt = shared_tiles;
+      kt.uniform();
+      const int qs = seg_start(a, qr), low = max(qs, qr - a.window + 1);
+#pragma unroll 1
+      for (int it = 0; it < kt.n; ++it) {
+        const int k0 = kt.first(it), k1 = min(k0 + kTR, kt.rows(it));
+        const Seen seen(kt, it, k0, qr, qs, low, a.n_sink, half);
+#pragma unroll 1
+        for (int k = k0; k < k1; ++k) {
+          const bf16_t *krow = kbase + (int64_t)k * ld;
+          const float p = fast_exp2(fmaf(row_dot<HD>(krow, qf, half), c, -lse));
+          const float ds = p * (row_dot<HD>(vbase + (int64_t)k * ld, df, half) + ndlt);
+          row_add<HD>(acc, krow, ds, qv & seen.template has<WIN>(k - k0 - 4 * half), half);
+        }
+      }
+    }
+  }
   if (!qv) return;
-  bf16_t *out = (bf16_t *)a.dqkv + (int64_t)q * ld + h * HD;
+  // (q's offset again: kept over the loop, it spills)
+  bf16_t *out = (bf16_t *)a.dqkv + (int64_t)(WIN ? opaque(q) : q) * ld + h * HD;
 #pragma unroll
   for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -1106,6 +1211,26 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
     }
     tail(Ci<2>{});
   }
+  if constexpr (WIN) {
+    if (__builtin_amdgcn_ballot_w64(kvv && (nonfinite(dk) | nonfinite(dv)))) {
+      const int half = opaque(hl);
+      clear(dk);
+      clear(dv);
+      const int q1 = wave_max(ke);
+#pragma unroll 1
+      for (int h = h0; h < h0 + n_h; ++h)
+#pragma unroll 1
+        for (int q = k0 + 32 * w; q < q1; ++q) {
+          const bf16_t *qrow = qkv + (int64_t)q * ld + h * HD, *drow = dout + (int64_t)q * ldo + h * HD;
+          const int64_t at = (int64_t)h * a.n_tok + q;
+          const float p = fast_exp2(fmaf(row_dot<HD>(qrow, kf, half), c, -a.lse[at]));
+          const float ds = p * (row_dot<HD>(drow, vf, half) + a.delta[at]);
+          const bool in = kvv & (q >= kv) & (q < ke);
+          row_add<HD>(dv, drow, p, in, half);
+          row_add<HD>(dk, qrow, ds, in, half);
+        }
+    }
+  }
   if (!kvv) return;
   if (parts > 1) {   // float32 sums of the part's heads, for attn_dkv_parts_kernel
     float *p = a.part + ((int64_t)part * a.n_tok + kv) * (2 * a.Hkv * HD) + g * HD;
@@ -1254,6 +1379,23 @@ __global__ __launch_bounds__(256, 1) void attn_sinks_mfma_kernel(WinAttnBwdArgs 
   for (int b = w; b < n_blk; b += 8) {
     block(b, 0);
     if (b + 4 < n_blk) block(b + 4, 1);
+  }
+  if (__builtin_amdgcn_ballot_w64(kvv && (nonfinite(dk) | nonfinite(dv)))) {
+    const int half = opaque(hl);
+    clear(dk);
+    clear(dv);
+#pragma unroll 1
+    for (int b = w; b < n_blk; b += 4)
+#pragma unroll 1
+      for (int q = qt0 + 32 * b; q < min(qt0 + 32 * b + 32, q_hi); ++q) {
+        const bf16_t *qrow = q_src + (int64_t)q * ld, *drow = d_src + (int64_t)q * ldo;
+        const int64_t at = (int64_t)h * a.n_tok + q;
+        const float p = fast_exp2(fmaf(row_dot<HD>(qrow, kf, half), c, -a.lse[at]));
+        const float ds = p * (row_dot<HD>(drow, vf, half) + a.delta[at]);
+        const bool in = kvv & (q >= kv);
+        row_add<HD>(dv, drow, p, in, half);
+        row_add<HD>(dk, qrow, ds, in, half);
+      }
   }
   __syncthreads();
   float *mine = (float *)sm[w] + lq * 2 * HD;

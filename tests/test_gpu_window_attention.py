@@ -1,9 +1,11 @@
 """Windowed attention with sinks against its definition in 64 bits (tests/window_attention.py),
 within the error that its roundings allow; what it leaves alone, and what it refuses."""
+import math
+
 import pytest
 import torch
 
-from window_attention import reference
+from window_attention import reference, visible
 
 pytestmark = pytest.mark.gpu
 
@@ -36,7 +38,7 @@ CASES = [
 ]
 
 
-def call(lens, hq, hkv, hd, window, n_sink, dtype, base=0, seed=0, scale=0.0, std=1.0):
+def call(lens, hq, hkv, hd, window, n_sink, dtype, base=0, seed=0, scale=0.0, std=1.0, bad=None):
     from paper_2606_04484_amd import capi
     g = torch.Generator().manual_seed(seed)
     n = sum(lens)
@@ -49,9 +51,12 @@ def call(lens, hq, hkv, hd, window, n_sink, dtype, base=0, seed=0, scale=0.0, st
     out = torch.full((n, hq * hd), float("nan"), dtype=dtype, device=dev)
     lse = torch.full((hq, n), float("nan"), device=dev)
     dqkv = torch.full((n, (hq + 2 * hkv) * hd), float("nan"), dtype=dtype, device=dev)
-    capi.aj_attention_fwd(cfg, cu, max(lens), qkv.to(dev), out, lse, ws, base=base)
+    x, dx = qkv.to(dev), dout.to(dev)
+    if bad is not None:      # (rows, value): in the operands, not in what is returned
+        x[bad[0]] = dx[bad[0]] = bad[1]
+    capi.aj_attention_fwd(cfg, cu, max(lens), x, out, lse, ws, base=base)
     ws.fill_(255)
-    capi.aj_attention_bwd(cfg, cu, max(lens), qkv.to(dev), out, lse, dout.to(dev), dqkv, ws, base=base)
+    capi.aj_attention_bwd(cfg, cu, max(lens), x, out, lse, dx, dqkv, ws, base=base)
     torch.cuda.synchronize()
     return qkv, dout, {"out": out.cpu(), "lse": lse.cpu(), "dqkv": dqkv.cpu()}
 
@@ -200,3 +205,48 @@ def test_bad_rows_far_from_the_window_do_no_harm(dtype):
     # 64 + window rows, and by their neighbours in a workgroup of 256
     far = torch.cat([torch.arange(0, 44), torch.arange(301 + 64 + window + 256, n)])
     assert torch.equal(res[0][far], res[1][far])
+
+
+def touched(lens, window, n_sink, bad):
+    """Rows that see a bad one (themselves included), and rows that such a row sees."""
+    n = sum(lens)
+    see = torch.zeros(n, n, dtype=torch.bool)
+    a = 0
+    for L in lens:
+        see[a:a + L, a:a + L] = visible(L, window, n_sink)
+        a += L
+    q = see[:, bad].any(1)
+    return q, see[q].any(0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf], ids=["nan", "+inf", "-inf"])
+@pytest.mark.parametrize("case", [
+    # lens, hq, hkv, hd, window, sinks, bad rows
+    ([200, 90, 150], 4, 2, 64, 20, 3, [70, 120, 289]),
+    ([200, 90, 150], 2, 1, 128, 20, 3, list(range(200, 290))),     # a segment that nothing wrote
+    ([31, 300], 7, 1, 128, 65, 0, [31, 32, 100, 330]),
+    ([2500, 40], 2, 1, 128, 50, 4, [1300, 2499]),                  # far sinks' chunks
+    ([1300, 33, 1100], 2, 2, 64, 30, 70, [1299, 1300, 1400]),
+    ([300, 60], 2, 1, 32, 20, 3, [299, 310]),
+], ids=lambda c: "x".join(map(str, c[0])) + "-hd%d" % c[3])
+def test_bad_rows_stay_with_the_rows_that_see_them(case, value, dtype):
+    """Infinities and NaN in a row, and in its output gradient, leave every result that does not
+    depend on that row what its definition says, in the same tile too."""
+    lens, hq, hkv, hd, window, n_sink, bad = case
+    qkv, dout, got = call(*case[:6], dtype, seed=4, bad=(bad, value))
+    q, k = touched(lens, window, n_sink, bad)
+    assert not q.all() and not (q | k).all()
+    for name, (val, err) in reference(qkv, lens, hq, hkv, hd, window, n_sink, dout,
+                                      bf16=dtype == torch.bfloat16).items():
+        rows = [(got[name], val, err, q)]
+        if name == "lse":
+            rows = [(got[name].T, val.T, err.T, q)]
+        elif name == "dqkv":
+            rows = [(t[0], t[1], t[2], m) for t, m in zip(
+                zip(*(x.split([hq * hd, 2 * hkv * hd], 1) for x in (got[name], val, err))), (q, k))]
+        for part, (have, want, room, skip) in enumerate(rows):
+            have, want, room = have[~skip], want[~skip], room[~skip]
+            assert bool(torch.isfinite(have).all()), (name, part)
+            worst = ((have.double() - want).abs() / (room + 1e-30)).max().item()
+            assert worst <= 1.0, (name, part, worst)
