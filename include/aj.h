@@ -557,8 +557,10 @@ int aj_distill_loss_fwd_bwd(const aj_logits *lg, const aj_teacher *t, float *los
  *   _topk: the teacher's lists; forward only.
  *   _distill: the student's loss and its whole backward: dh float32 [n_tok, d] WRITTEN
  * (rows that feed no target become 0), d_final_norm [d] and d_w_vocab [vocab, d]
- * accumulated, NULL where frozen.  loss [n_tgt]; stats as above, or NULL.
- * err: AJ_DEVERR_OFFSETS for a target outside the pack, and the lists' errors.
+ * accumulated, NULL where frozen.  loss [n_tgt]; stats as above, or NULL.  The targets
+ * ascend, each once.
+ * err: AJ_DEVERR_OFFSETS for a target outside the pack (for _distill also for one that
+ * is not above the one before: of two in one row dh keeps either), and the lists' errors.
  * ws: aj_lm_head_workspace_bytes(cfg, n_tgt, k): the logits of a slab (4 bytes each; with
  * bfloat16 2 more for d logits) and 134 MB at most for split reductions. */
 size_t aj_lm_head_workspace_bytes(const aj_loss_cfg *cfg, int32_t n_tgt, int32_t k);

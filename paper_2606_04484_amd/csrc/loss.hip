@@ -108,12 +108,14 @@ AJ_DEV float wave_sum(float v) {
 }
 
 // Target p is scored from h row p - 1 - row_base; anything outside [0, n_tok)
-// is reported and clamped so that no access leaves the documented ranges.
+// is reported and clamped so that no access leaves the documented ranges.  `ascending`:
+// so is a target not above the one before (each writes its own row of dh).
 __global__ void sanitize_targets_kernel(int n, const int32_t *targets, int row_base, int n_tok,
-                                        int32_t *tpos, int32_t *trow, int32_t *err) {
+                                        int32_t *tpos, int32_t *trow, int32_t *err, bool ascending) {
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= n) return;
   int r = targets[i] - 1 - row_base;
+  if (ascending && i > 0 && targets[i] <= targets[i - 1] && err) atomicOr(err, AJ_DEVERR_OFFSETS);
   if (r < 0 || r >= n_tok) {
     if (err) atomicOr(err, AJ_DEVERR_OFFSETS);
     r = r < 0 ? 0 : n_tok - 1;
@@ -602,7 +604,7 @@ int loss_fwd(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, const vo
              int32_t *err, const LossWs &w, hipStream_t st) {
   const int n = in.n_tgt, d = c.d_model;
   sanitize_targets_kernel<<<(n + 255) / 256, 256, 0, st>>>(n, in.targets, in.row_base, in.n_tok,
-                                                           w.tpos, w.trow, err);
+                                                           w.tpos, w.trow, err, false);
   aj::rmsnorm_fwd<T>((const T *)h, (const T *)gf, n, d, c.rms_eps, w.trow, 0, (T *)sv.hn,
                      sv.rstd, st);
   const bool fused = sizeof(T) == 2;
@@ -651,7 +653,7 @@ int loss_bwd(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, const vo
   aj::fill_f32(dh, (int64_t)in.n_tok * d, 0.f, st);
   if (n == 0) return aj::check_launch("aj_logprob_pg_loss_bwd");
   sanitize_targets_kernel<<<(n + 255) / 256, 256, 0, st>>>(n, in.targets, in.row_base, in.n_tok,
-                                                           w.tpos, w.trow, nullptr);
+                                                           w.tpos, w.trow, nullptr, false);
   const float *ref = in.kl_coef != 0.f ? in.ref_logprob : nullptr;
   loss_grad_kernel<<<(n + 255) / 256, 256, 0, st>>>(n, w.tpos, logprob, in.old_logprob, in.adv,
                                                     c.clip_eps, in.inv_n_mask, ref, in.kl_coef,
@@ -779,9 +781,9 @@ int check_head(const aj_loss_cfg *c, const aj_loss_in *in, int k, float inv_temp
 // The targets' normalised rows.
 template <typename T>
 void head_rows(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, const void *gf, const HeadWs &w,
-               int32_t *err, hipStream_t st) {
+               int32_t *err, bool ascending, hipStream_t st) {
   sanitize_targets_kernel<<<(in.n_tgt + 255) / 256, 256, 0, st>>>(in.n_tgt, in.targets, in.row_base, in.n_tok,
-                                                                  w.tpos, w.trow, err);
+                                                                  w.tpos, w.trow, err, ascending);
   aj::rmsnorm_fwd<T>((const T *)h, (const T *)gf, in.n_tgt, c.d_model, c.rms_eps, w.trow, 0, (T *)w.hn, w.rstd, st);
 }
 
@@ -802,7 +804,7 @@ template <typename T>
 int head_topk(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, const void *gf, const void *w_vocab,
               float inv_temp, int k, int32_t *idx, float *logprob, float *lse, int32_t *err, const HeadWs &w,
               hipStream_t st) {
-  head_rows<T>(c, in, h, gf, w, err, st);
+  head_rows<T>(c, in, h, gf, w, err, false, st);
   for (int r0 = 0; r0 < in.n_tgt; r0 += kHeadSlab) {
     const int n = std::min(kHeadSlab, in.n_tgt - r0);
     int r;
@@ -822,7 +824,7 @@ int head_distill(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, cons
   const int d = c.d_model;
   aj::fill_f32(dh, (int64_t)in.n_tok * d, 0.f, st);
   if (in.n_tgt == 0) return aj::check_launch("aj_lm_head_distill");
-  head_rows<T>(c, in, h, gf, w, err, st);
+  head_rows<T>(c, in, h, gf, w, err, true, st);
   aj::fill_f32(w.dhn, (int64_t)in.n_tgt * d, 0.f, st);
   for (int r0 = 0; r0 < in.n_tgt; r0 += kHeadSlab) {
     const int n = std::min(kHeadSlab, in.n_tgt - r0);
