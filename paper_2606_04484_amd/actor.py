@@ -371,6 +371,8 @@ class ActorUpdate:
         if tuple(idx.shape) != tuple(logprob.shape) or idx.shape[0] != L.n_mask:
             raise C.AjError(f"distill_step: lists {tuple(idx.shape)}, {tuple(logprob.shape)} for "
                             f"{L.n_mask} targets")
+        if weight is not None and tuple(weight.shape) != (L.n_mask,):
+            raise C.AjError(f"distill_step: weight {tuple(weight.shape)} for {L.n_mask} targets")
         self._head_buffers(L, idx.shape[1])
         if coef is None:
             coef = 1.0 / L.n_mask if L.n_mask else 0.0

@@ -690,7 +690,8 @@ def aj_lm_head_topk(cfg, targets, h, final_norm, w_vocab, inv_temp, idx, logprob
     a = _head(name, cfg, targets, h, final_norm, w_vocab, row_base, w_vocab_t)
     n, k = a.n_tgt, idx.shape[1]
     _operands(name, {"idx": (idx, (torch.int32,), (n, k)), "logprob": (logprob, (torch.float32,), (n, k)),
-                     "lse": (lse, (torch.float32,), (n,))})
+                     "lse": (lse, (torch.float32,), (n,)),
+                     **({} if err is None else {"err": (err, (torch.int32,), (1,))})})
     _check(lib().aj_lm_head_topk(C.byref(cfg), C.byref(a), ptr(h), ptr(final_norm), ptr(w_vocab), inv_temp, k,
                                  ptr(idx), ptr(logprob), ptr(lse), ptr(err), *_workspace(name, ws),
                                  stream_handle(stream)), name)
@@ -706,8 +707,9 @@ def aj_lm_head_distill(cfg, targets, h, final_norm, w_vocab, inv_temp, t, loss, 
     idx, logprob, weight = t.tensors
     ops = {"idx": (idx, (torch.int32,), (n, t.k)), "logprob": (logprob, f, (n, t.k)), "weight": (weight, f, (n,)),
            "loss": (loss, f, (n,)), "dh": (dh, f, tuple(h.shape)), "d_final_norm": (d_final_norm, f, (cfg.d_model,)),
-           "d_w_vocab": (d_w_vocab, f, (cfg.vocab, cfg.d_model)), "stats": (stats, f, (2,))}
-    optional = ("weight", "d_final_norm", "d_w_vocab", "stats")
+           "d_w_vocab": (d_w_vocab, f, (cfg.vocab, cfg.d_model)), "stats": (stats, f, (2,)),
+           "err": (err, (torch.int32,), (1,))}
+    optional = ("weight", "d_final_norm", "d_w_vocab", "stats", "err")
     _operands(name, {k: v for k, v in ops.items() if v[0] is not None or k not in optional})
     _check(lib().aj_lm_head_distill(C.byref(cfg), C.byref(a), ptr(h), ptr(final_norm), ptr(w_vocab), inv_temp,
                                     C.byref(t), ptr(loss), ptr(stats), ptr(dh), ptr(d_final_norm), ptr(d_w_vocab),

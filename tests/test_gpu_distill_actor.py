@@ -131,3 +131,18 @@ def test_update_with_adapters_and_after_a_step():
     torch.cuda.synchronize()
     for k, g in A.G.items():
         assert torch.equal(g, first[k]), k
+
+
+def test_weights_of_another_layout_are_refused_before_any_work():
+    from paper_2606_04484_amd import actor, capi
+    case = Case(workload(TINY))
+    L = actor.merge(actor.upload_timelines(case.tl, case.old), pack_tokens=700)
+    A = actor.ActorUpdate(case.m, case.device_weights())
+    A.zero_grads()
+    idx, lp = A.teacher_topk(L, 8)
+    with pytest.raises(capi.AjError, match="weight"):
+        A.distill_step(L, idx, lp, weight=torch.ones(L.n_mask - 1, device="cuda"))
+    with pytest.raises(capi.AjError, match="lists"):
+        A.distill_step(L, idx[1:], lp[1:])
+    torch.cuda.synchronize()
+    assert all(not bool(g.any()) for g in A.G.values())

@@ -131,3 +131,23 @@ def test_reported_targets(dtype):
         keep = torch.arange(20) != at
         assert got[5] != 0 and torch.equal(got[0][keep], want[0][keep]), (at, int(value))
     assert math.isfinite(want[0].sum())
+
+
+def test_operands_of_the_head():
+    from paper_2606_04484_amd import capi
+    cfg, h, gamma, w, rows, targets = setup(50, 20, torch.float32, seed=2)
+    f = lambda *s, dt=torch.float32: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
+    ws = f(capi.aj_lm_head_workspace_bytes(cfg, 20, 5), dt=torch.uint8)
+    lists_ = f(20, 5, dt=torch.int32), f(20, 5)
+    args = [targets.cuda(), h.cuda(), gamma.cuda(), w.cuda(), 1.0]
+    t = capi.teacher(*lists_)
+    for what, bad in (("err", f(1)), ("err", f(2, dt=torch.int32)), ("err", torch.zeros(1, dtype=torch.int32))):
+        with pytest.raises(capi.AjError, match=what):
+            capi.aj_lm_head_topk(cfg, *args, *lists_, f(20), ws, row_base=BASE, err=bad)
+        with pytest.raises(capi.AjError, match=what):
+            capi.aj_lm_head_distill(cfg, *args, t, f(20), f(50, D), None, None, ws, row_base=BASE, err=bad)
+    with pytest.raises(capi.AjError, match="dh"):
+        capi.aj_lm_head_distill(cfg, *args, t, f(20), f(49, D), None, None, ws, row_base=BASE)
+    with pytest.raises(capi.AjError, match="weight"):
+        capi.aj_lm_head_distill(cfg, *args, capi.teacher(*lists_, weight=f(19)), f(20), f(50, D), None, None, ws,
+                                row_base=BASE)
