@@ -140,6 +140,7 @@ struct WinAttnBwdArgs : AttnBwdArgs {
   int window = 0, n_sink = 0;   // as the forward's
   bool lse_log2 = false;
   float *sink_part = nullptr;   // scratch for the sinks' sums, attn_sink_floats of it
+  bool few = false;             // the windowed kernels also where the window hides nothing
   explicit WinAttnBwdArgs(const AttnBwdArgs &a) : AttnBwdArgs(a) {}
 };
 template <typename T>

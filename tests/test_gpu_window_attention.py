@@ -250,3 +250,23 @@ def test_bad_rows_stay_with_the_rows_that_see_them(case, value, dtype):
             assert bool(torch.isfinite(have).all()), (name, part)
             worst = ((have.double() - want).abs() / (room + 1e-30)).max().item()
             assert worst <= 1.0, (name, part, worst)
+
+
+@pytest.mark.parametrize("case", [([130, 3], 4, 2, 64, 1, 0), ([300], 2, 1, 128, 1, 0), ([1], 4, 2, 128, 0, 0),
+                                  ([1] * 70, 4, 2, 64, 0, 0), ([1] * 90, 7, 1, 128, 30, 4)],
+                         ids=lambda c: "%dx%d-w%d-hd%d" % (len(c[0]), c[0][0], c[4], c[3]))
+def test_rows_of_one_key_pass_no_gradient_to_scores(case):
+    """p = 1 and dP = delta: d q and d k are what float32 leaves of their difference, not the
+    rounding of a bfloat16 output."""
+    lens, hq, hkv, hd, window, n_sink = case
+    qkv, dout, got = call(*case, torch.bfloat16, seed=6)
+    n, G, c = sum(lens), hq // hkv, 1.0 / math.sqrt(hd)
+    q, k, v = (t.reshape(n, -1, hd).abs() for t in qkv.double().split([hq * hd, hkv * hd, hkv * hd], 1))
+    k, v = k.repeat_interleave(G, 1), v.repeat_interleave(G, 1)
+    d = dout.double().reshape(n, hq, hd).abs()
+    # dP twice, hd products each; p, the exponential of a score less its log-sum-exp, by its own error
+    size = c * (q * k).sum(2)
+    ds = 2.0 ** -24 * (2 * (hd + 4) + 4 * (hd + 6) * size + 16) * (d * v).sum(2)
+    room = torch.cat([(ds[..., None] * k * c).reshape(n, -1),
+                      (ds[..., None] * q * c).reshape(n, hkv, G, hd).sum(2).reshape(n, -1)], 1) * (1 + 2.0 ** -7)
+    assert bool((got["dqkv"][:, :(hq + hkv) * hd].double().abs() <= room).all())
