@@ -676,9 +676,10 @@ int check_attn(const aj_attn_cfg *c, const aj_varlen *v, const char *name) {
   return AJ_OK;
 }
 
-// Rows of a pack up to which every workgroup of the windowed dQ has few tiles.  Forward and
-// backward, windowed kernels against causal ones: 15 tokens of 12 heads 36 us against 39, 200
-// tokens 51 against 47.
+// Rows of a pack up to which every workgroup of the windowed dQ has few tiles; so have nearly
+// all where segments are half as long.  Forward and backward, windowed kernels against
+// causal ones, us: 15 tokens of 12 heads of 128 36 / 39, 200 tokens 51 / 47, 900 in 9 segments
+// 69 / 63; 20000 of 28 heads in 500 segments 646 / 667, in 160 737 / 778 (of 64 457 / 455).
 constexpr int kFewRows = 256;
 
 float attn_scale(const aj_attn_cfg &c) {
@@ -727,8 +728,9 @@ extern "C" int aj_attention_bwd(const aj_attn_cfg *cfg, const aj_varlen *vl, con
   a.window = cfg->window;
   a.n_sink = cfg->n_sink;
   a.lse_log2 = true;
-  // packs that are all early rows: the windowed dQ, whose delta is exact there
-  if (vl->n_tok <= aj::kFewRows && !aj::windowed(a.window, a.n_tok)) {
+  // packs of early rows: the windowed dQ, whose delta is exact there
+  if (!aj::windowed(a.window, a.n_tok) &&
+      (a.n_tok <= aj::kFewRows || a.n_tok / a.n_seg <= aj::kFewRows / 2)) {
     a.few = true;
     a.window = a.n_tok;
   }
