@@ -676,10 +676,11 @@ int check_attn(const aj_attn_cfg *c, const aj_varlen *v, const char *name) {
   return AJ_OK;
 }
 
-// Rows of a pack up to which every workgroup of the windowed dQ has few tiles; so have nearly
-// all where segments are half as long.  Forward and backward, windowed kernels against
-// causal ones, us: 15 tokens of 12 heads of 128 36 / 39, 200 tokens 51 / 47, 900 in 9 segments
-// 69 / 63; 20000 of 28 heads in 500 segments 646 / 667, in 160 737 / 778 (of 64 457 / 455).
+// Mean rows of a segment up to which a pack is one of early rows: most workgroups of the
+// windowed dQ then have few tiles.  Forward and backward, windowed kernels against causal
+// ones, us: 15 tokens of 12 heads of 128 36 / 39, 200 tokens 51 / 47, 900 in 9 segments 69 / 63;
+// 20000 of 28 heads in 500 segments 646 / 667, in 160 737 / 778 (of 64 457 / 455), in 80
+// 883 / 938 (of 64 559 / 571).
 constexpr int kFewRows = 256;
 
 float attn_scale(const aj_attn_cfg &c) {
@@ -729,8 +730,7 @@ extern "C" int aj_attention_bwd(const aj_attn_cfg *cfg, const aj_varlen *vl, con
   a.n_sink = cfg->n_sink;
   a.lse_log2 = true;
   // packs of early rows: the windowed dQ, whose delta is exact there
-  if (!aj::windowed(a.window, a.n_tok) &&
-      (a.n_tok <= aj::kFewRows || a.n_tok / a.n_seg <= aj::kFewRows / 2)) {
+  if (!aj::windowed(a.window, a.n_tok) && a.n_tok / a.n_seg <= aj::kFewRows) {
     a.few = true;
     a.window = a.n_tok;
   }
