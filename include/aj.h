@@ -494,6 +494,10 @@ int aj_logprob_pg_loss_bwd(const aj_loss_cfg *cfg, const aj_loss_in *in, const v
  * them once or, with the gradient, twice, and does all sums of a row over its
  * parts in float32 and over the parts in 64 bits, in one fixed order
  * (bit-identical on every call).
+ * Finite logits of any size count as they are (a row masked with the type's lowest value is
+ * uniform): sums are relative to their largest value.  A log-sum-exp that is finite and
+ * beyond float32's range is stored as float32's lowest or largest value; -inf is that of
+ * nothing but -inf.
  */
 typedef struct {
   int32_t rows, vocab;          /* vocab at most 2^24 */
@@ -533,7 +537,8 @@ typedef struct {
  *   loss[row] = sum_k p_k (log p_k - log q_k) + p_rest (log p_rest - log q_rest)
  * (0 for a row with nothing listed; not scaled by weight or coef).  lse: [2, rows], the
  * log-sum-exp of the row's logits * inv_temp and that of the tokens not listed; the
- * backward reads it.  stats (may be NULL): float32[2] accumulated: [0] the sum of
+ * backward reads it, and sums a row again where one it needs is 16384 or more (float32
+ * would be off by 2^-10 and more).  stats (may be NULL): float32[2] accumulated: [0] the sum of
  * coef * weight * loss, [1] rows.  ws: aj_distill_workspace_bytes for at least these rows.
  * The gradient, d logits [rows, vocab] in d_dtype with row stride ldd, is WRITTEN:
  *   coef * weight * inv_temp * (M q_v - p_v),  M = sum p + p_rest,

@@ -6,6 +6,7 @@
 // 16-byte boundary: its values are numbered from the boundary before it (u = v + shift),
 // so that every thread's run of 16 bytes is aligned and only the row's first and last runs
 // are guarded value by value.
+#include <cfloat>
 #include <algorithm>
 #include <type_traits>
 #include "ops.h"
@@ -13,7 +14,7 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr double kLog2eD = 1.4426950408889634074, kLn2D = 0.69314718055994530942;
+constexpr double kLog2eD = 1.4426950408889634074;
 constexpr int kMaxK = 256;
 
 // 2^x on the hardware unit for x <= 0 or -inf (values under 2^-126 come out 0)
@@ -30,6 +31,59 @@ template <typename V> AJ_DEV V wave_sum(V v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
+}
+
+// Sums of 2^((z - m) c) over values z, m the largest of them.  The unit is a value and not
+// its product with c, which finite values may take out of float32's range (a vocabulary masked
+// with the lowest value, a low temperature); and the difference is formed of halves, as that
+// of two finite values may be.  c2 = 2 c, c = inv_temp log2(e).
+AJ_DEV float half_unit(float m) { return m == -INFINITY ? 0.f : 0.5f * m; }
+AJ_DEV float below(float z, float half, float c2) { return fmaf(z, 0.5f, -half) * c2; }
+// s of unit m in the unit `half` (of a value not below m); a NaN stays one
+AJ_DEV float in_unit(float m, float s, float half, float c2) {
+  return m == -INFINITY ? (s == s ? 0.f : s) : s * fast_exp2(below(m, half, c2));
+}
+struct RunSum {
+  float m = -INFINITY, s = 0.f;
+  // the values z, the largest of which is `top`
+  template <int N> AJ_DEV void add(const float (&z)[N], float top, float c2) {
+    const float up = fmaxf(m, top), half = half_unit(up);
+    s = in_unit(m, s, half, c2);
+    m = up;
+#pragma unroll
+    for (int e = 0; e < N; ++e) s += fast_exp2(below(z[e], half, c2));
+  }
+  template <int N> AJ_DEV void add(const float (&z)[N], float c2) {
+    float top = z[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
+    add(z, top, c2);
+  }
+};
+// Parts' sums (m, s) in 64 bits, one wave's or one thread's share of them: in the unit M.
+AJ_DEV double part_in_unit(float2 p, double M, double c) {
+  return p.x == -INFINITY && p.y == 0.f ? 0.0 : (double)p.y * exp2(((double)p.x - M) * c);
+}
+
+// A natural log of a sum as unit + log, apart: the unit may be so large that their sum leaves
+// nothing of log.  log -inf: the sum of nothing.
+struct LogSum {
+  double unit, log;
+  AJ_DEV bool none() const { return log == -INFINITY; }
+};
+AJ_DEV LogSum log_of(double m, double s, double inv_temp) { return {m == -INFINITY ? 0.0 : m * inv_temp, log(s)}; }
+AJ_DEV LogSum join(const LogSum &a, const LogSum &b) {
+  if (a.none()) return b;
+  if (b.none()) return a;
+  const double hi = max(a.unit, b.unit);
+  return {hi, log(exp(a.unit - hi + a.log) + exp(b.unit - hi + b.log))};
+}
+// log of a's sum over b's
+AJ_DEV double log_ratio(const LogSum &a, const LogSum &b) { return (a.unit - b.unit) + (a.log - b.log); }
+// as a result: -inf of nothing only
+AJ_DEV float as_float(const LogSum &a) {
+  const double v = a.unit + a.log;
+  return a.none() ? -INFINITY : v != v ? (float)v : (float)min(max(v, -(double)FLT_MAX), (double)FLT_MAX);
 }
 
 // LDS writes (or reads) complete, then a barrier.  __syncthreads would wait for the loads
@@ -265,25 +319,21 @@ AJ_DEV void write_ranked(const WaveList &l, uint64_t (*lists)[kWaveCap + kRankPa
 // A row's results from its k largest places and its log-sum-exp.
 template <typename T>
 AJ_DEV void write_row(const void *logits, int64_t ld, int64_t row, int k, double inv_temp, const uint64_t *ranked,
-                      double l, int32_t *idx, float *logprob, float *lse) {
+                      const LogSum &l, int32_t *idx, float *logprob, float *lse) {
   const int i = threadIdx.x;
   if (i < k) {
     const int id = place_index(ranked[i]);
     const double z = ldf((const T *)logits + row * ld + id);
     idx[row * k + i] = id;
     // a row of nothing but -inf has no probabilities: -inf for each
-    logprob[row * k + i] = l == -INFINITY ? -INFINITY : (float)(z * inv_temp - l);
+    logprob[row * k + i] = l.none() ? -INFINITY : (float)((z * inv_temp - l.unit) - l.log);
   }
-  if (i == 0) lse[row] = (float)l;
-}
-// natural log of a sum given as a power of two and a factor
-AJ_DEV double log_of(double power, double sum) {
-  return power == -INFINITY && sum == 0.0 ? -INFINITY : (power + log2(sum)) * kLn2D;
+  if (i == 0) lse[row] = as_float(l);
 }
 
 // One workgroup per part [u0, u0 + width) of a row, kTopChunk values at a time, the next
 // ones on their way meanwhile.  Gives the part's k largest places in order (0 after the
-// last), and its sum of 2^(z c) as a power of two (log2 units) and a factor.
+// last), and its sum of 2^((z - m) c) with m.
 //
 // Values not below a threshold that k of those met so far reach go to a list in LDS.
 // The first threshold comes from the threads' maxima (two each): in every wave the
@@ -302,7 +352,7 @@ __global__ __launch_bounds__(kTopNT, 5) void topk_part_kernel(
   __shared__ float red_m[kTopWaves], red_s[kTopWaves];
   __shared__ uint32_t red_t[kTopWaves];
   __shared__ int red_i[3][kTopWaves], red_n[3][kTopWaves];
-  const float c = inv_temp * kLog2e;
+  const float c2 = 2.f * inv_temp * kLog2e;
   const int64_t row = blockIdx.x / parts;
   const int part = blockIdx.x % parts;
   const Row<T> x(logits, row, ld, vocab);
@@ -326,7 +376,7 @@ __global__ __launch_bounds__(kTopNT, 5) void topk_part_kernel(
   WaveList list{lists[wave], 0};
   uint64_t least = 0;         // the least place that goes to a list
   float tau = -INFINITY;      // ... and its value
-  float ref = -INFINITY, s = 0.f;
+  RunSum sum;
   int turn = 0;
   for (int u = u0; u < u1; u += C) {
     float z[E];
@@ -348,14 +398,9 @@ __global__ __launch_bounds__(kTopNT, 5) void topk_part_kernel(
       if (q & 1) m1 = fmaxf(m1, top[q]);
       else m0 = fmaxf(m0, top[q]);
     }
-    // s counts in units of 2^ref, ref the rounded product of the largest value and c
-    const float up = fmaxf(ref, fmaxf(m0, m1) * c), base = up == -INFINITY ? 0.f : up;
-    s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
-    ref = up;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += fast_exp2(fmaf(z[e], c, -base));
+    sum.add(z, fmaxf(m0, m1), c2);
     if (first) {
-      s += fast_exp2(fmaf(zr, c, -base));
+      sum.s += fast_exp2(below(zr, half_unit(sum.m), c2));
       const uint32_t o0 = order_bits(m0), o1 = order_bits(m1);
       const int j = (k + kTopWaves - 1) / kTopWaves;
       uint32_t t = 0;
@@ -386,7 +431,7 @@ __global__ __launch_bounds__(kTopNT, 5) void topk_part_kernel(
     const uint64_t pr = first && rim >= 0 ? place(zr, rim - x.shift) : 0;
     // a thread whose sum is NaN has met a NaN (which no maximum shows) or +inf: it
     // looks at all it holds
-    float bar = s == s ? tau : -INFINITY;
+    float bar = sum.s == sum.s ? tau : -INFINITY;
     int had = list.n, n;
     for (;;) {
 #pragma unroll
@@ -425,18 +470,18 @@ __global__ __launch_bounds__(kTopNT, 5) void topk_part_kernel(
   lds_barrier();
   const int n = waves_sum(list.n, red_n[0]);
   if (n > k + 128) cut(list, k, k + kSlack, least, red_i);
-  const float wm = wave_max(ref);
+  const float wm = wave_max(sum.m);
   if (lane == 0) red_m[wave] = wm;
   __syncthreads();
   const float M = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
-  s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - M));
+  const float s = wave_sum(in_unit(sum.m, sum.s, half_unit(M), c2));
   if (lane == 0) red_s[wave] = s;
   if ((int)threadIdx.x < k) ranked[threadIdx.x] = 0;
   write_ranked(list, lists, k, ranked, red_i[0]);
   __syncthreads();
   const float S = red_s[0] + red_s[1] + red_s[2] + red_s[3];
   if (parts == 1) {
-    write_row<T>(logits, ld, row, k, inv_temp, ranked, log_of(M, S), idx, logprob, lse);
+    write_row<T>(logits, ld, row, k, inv_temp, ranked, log_of(M, S, inv_temp), idx, logprob, lse);
     return;
   }
   if ((int)threadIdx.x < k) cand[(int64_t)blockIdx.x * k + threadIdx.x] = ranked[threadIdx.x];
@@ -497,8 +542,7 @@ __global__ __launch_bounds__(kMergeNT) void topk_merge_kernel(const void *logits
   uint64_t t = max(max(lo, hi), (uint64_t)1);   // (0 is no place)
   // the row's log-sum-exp in 64 bits from the parts' sums
   double s = 0.0;
-  for (int q = threadIdx.x; q < parts; q += kMergeNT)
-    s += p[q].x == -INFINITY && p[q].y == 0.f ? 0.0 : (double)p[q].y * exp2((double)p[q].x - M);
+  for (int q = threadIdx.x; q < parts; q += kMergeNT) s += part_in_unit(p[q], M, inv_temp * kLog2eD);
   s = wave_sum(s);
   if (lane == 0) red[wave] = s;
   __syncthreads();
@@ -517,7 +561,7 @@ __global__ __launch_bounds__(kMergeNT) void topk_merge_kernel(const void *logits
   lds_barrier();
   write_ranked(list, lists, k, ranked, red_i[0]);
   __syncthreads();
-  write_row<T>(logits, ld, row, k, inv_temp, ranked, log_of(M, s), idx, logprob, lse);
+  write_row<T>(logits, ld, row, k, inv_temp, ranked, log_of(M, s, inv_temp), idx, logprob, lse);
 }
 
 // ------------------------------------------------------------------ distillation
@@ -603,60 +647,60 @@ AJ_DEV Listed listed(const Teacher &t, int64_t row, int vocab, int32_t *err, int
   return e;
 }
 
-// Of a row's named values: their log-sum-exp and sum p (log p - z inv_temp).  (Known before
-// the others' sum is: what comes after that is on every row's critical path.)
-struct NamedSums { double list, term; };
+// Of a row's named values: their log-sum-exp and sum p (log p - (z inv_temp - its unit)).
+// (Known before the others' sum is: what comes after that is on every row's critical path.)
+struct NamedSums { LogSum list; double term; };
 template <int WAVES>
 AJ_DEV NamedSums named_sums(const Listed &e, double z, double inv_temp, double *red) {
-  const double c = inv_temp * kLog2eD, mz = block_max<WAVES>(z, red);
-  const double sz = block_sum<WAVES>(z == -INFINITY ? 0.0 : exp2((z - mz) * c), red);
+  const double top = block_max<WAVES>(z, red), m = top == -INFINITY ? 0.0 : top;
+  const double sz = block_sum<WAVES>(z == -INFINITY ? 0.0 : exp2((z - m) * (inv_temp * kLog2eD)), red);
   double term = 0.0;
-  if (e.p > 0.0 || e.p != e.p) term = e.p * (e.logp - z * inv_temp);
-  return {sz == 0.0 ? -INFINITY : (mz * c + log2(sz)) * kLn2D, block_sum<WAVES>(term, red)};
+  if (e.p > 0.0 || e.p != e.p) term = e.p * (e.logp - (z - m) * inv_temp);
+  return {log_of(m, sz, inv_temp), block_sum<WAVES>(term, red)};
 }
 
 // A row's log-sum-exps, of all values and of those not named, and its loss; in one wave.
-// ms: the sums of the values not named, as powers of two and factors.
-struct RowSums { double all, rest, loss; };
-AJ_DEV RowSums row_sums(const Listed &e, const NamedSums &n, const float2 *ms, int parts) {
+// ms: the sums of the values not named, with their units.
+struct RowSums { LogSum all, rest; double loss; };
+AJ_DEV RowSums row_sums(const Listed &e, const NamedSums &n, const float2 *ms, int parts, double inv_temp) {
   const int lane = threadIdx.x & 63;
   RowSums r;
-  double M = -INFINITY;
-  for (int q = lane; q < parts; q += 64) M = max(M, (double)ms[q].x);
+  float M = -INFINITY;
+  for (int q = lane; q < parts; q += 64) M = fmaxf(M, ms[q].x);
   M = wave_max(M);
   double s = 0.0;
-  for (int q = lane; q < parts; q += 64)
-    s += ms[q].x == -INFINITY && ms[q].y == 0.f ? 0.0 : (double)ms[q].y * exp2((double)ms[q].x - M);
-  s = wave_sum(s);
-  r.rest = log_of(M, s);
-  const double hi = max(r.rest, n.list);
-  r.all = r.rest + n.list;     // NaN where one is
-  if (r.all == r.all || hi == -INFINITY)
-    r.all = hi == -INFINITY ? -INFINITY : hi + log(exp(r.rest - hi) + exp(n.list - hi));
+  for (int q = lane; q < parts; q += 64) s += part_in_unit(ms[q], M, inv_temp * kLog2eD);
+  r.rest = log_of(M, wave_sum(s), inv_temp);
+  r.all = join(r.rest, n.list);
   r.loss = n.term;
   const double p = e.mass - e.rest;
-  if (p != 0.0) r.loss += p * r.all;
-  if (e.rest > 0.0) r.loss += e.rest * (log(e.rest) - (r.rest - r.all));
+  if (p != 0.0) r.loss += p * ((r.all.unit - n.list.unit) + r.all.log);
+  if (e.rest > 0.0) r.loss += e.rest * (log(e.rest) - log_ratio(r.rest, r.all));
   return r;
 }
 
-// The gradient of the values not named, 2^(z c - ref) f, and of a named one.
+// The gradient of the values not named, 2^((z - 2 half) c - more) f, and of a named one.
 struct RowGrad {
-  float c, ref, f;
+  float c2, half, more, f;
   int none;       // nothing listed: no loss, no gradient, whatever the logits
-  double w, all;
-  AJ_DEV void init(const Teacher &t, const Listed &e, double inv_temp, double weight, double all_, double rest) {
+  double w;
+  LogSum all;
+  AJ_DEV void init(const Teacher &t, const Listed &e, double inv_temp, double weight, const LogSum &all_,
+                   const LogSum &rest) {
     all = all_;
     w = (double)t.coef * inv_temp * weight;
-    const double l = t.tail ? rest : all;
-    ref = l == -INFINITY ? 0.f : (float)(l * kLog2eD);
-    c = (float)(inv_temp * kLog2eD);
-    f = (float)(t.tail ? w * (e.mass * exp(rest - all) - e.rest) : w * e.mass);
+    const LogSum &l = t.tail ? rest : all;
+    half = l.none() ? 0.f : (float)(0.5 * l.unit / inv_temp);
+    more = l.none() ? 0.f : (float)((l.unit - 2.0 * half * inv_temp + l.log) * kLog2eD);
+    c2 = (float)(2.0 * inv_temp * kLog2eD);
+    f = (float)(t.tail ? w * (e.mass * exp(log_ratio(rest, all)) - e.rest) : w * e.mass);
     none = e.mass == 0.0;
   }
-  AJ_DEV float other(float z) const { return none ? 0.f : fast_exp2(fmaf(z, c, -ref)) * f; }
+  AJ_DEV float other(float z) const {
+    return none ? 0.f : fast_exp2(fmaf(fmaf(z, 0.5f, -half), c2, -more)) * f;
+  }
   AJ_DEV float named(const Listed &e, double z, double inv_temp) const {
-    return none ? 0.f : (float)(w * (e.mass * exp(z * inv_temp - all) - e.p));
+    return none ? 0.f : (float)(w * (e.mass * exp((z * inv_temp - all.unit) - all.log) - e.p));
   }
 };
 
@@ -689,11 +733,11 @@ AJ_DEV void mark(uint32_t *bits, int v, int shift, int vocab, int u0, int u1) {
   if (u >= u0 && u < u1) atomicOr(&bits[(u - u0) >> 5], 1u << ((u - u0) & 31));
 }
 
-// One workgroup per part [u0, u1) of a row: the sum of 2^(z c) over the values that the list
-// does not name, as a power of two (log2 units) and a factor.
+// One workgroup per part [u0, u1) of a row: the sum of 2^((z - m) c) over the values that the
+// list does not name, with m.
 template <typename T>
 __global__ __launch_bounds__(kNT) void distill_part_kernel(const void *logits, int64_t ld, int vocab,
-                                                           int parts, int width, Teacher t, float c,
+                                                           int parts, int width, Teacher t, float c2,
                                                            float2 *ms) {
   constexpr int R = kRun<T>, kStep = kNT * R * kQ;
   __shared__ uint32_t bits[kSplit / 32];
@@ -709,8 +753,7 @@ __global__ __launch_bounds__(kNT) void distill_part_kernel(const void *logits, i
   __syncthreads();
   if ((int)threadIdx.x < t.k) mark(bits, t.idx[row * t.k + threadIdx.x], x.shift, vocab, u0, u1);
   __syncthreads();
-  // s counts in units of 2^ref, ref the rounded product of the largest value and c
-  float ref = -INFINITY, s = 0.f;
+  RunSum sum;
   for (int u = u0; u < u1; u += kStep) {
     float z[kQ * R];
 #pragma unroll
@@ -728,23 +771,15 @@ __global__ __launch_bounds__(kNT) void distill_part_kernel(const void *logits, i
       }
     }
     if (u + kStep < u1) fetch(u + kStep);
-    float n = z[0];
-#pragma unroll
-    for (int e = 1; e < kQ * R; ++e) n = fmaxf(n, z[e]);
-    n = fmaxf(ref, n * c);
-    const float base = n == -INFINITY ? 0.f : n;
-    s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
-    ref = n;
-#pragma unroll
-    for (int e = 0; e < kQ * R; ++e) s += fast_exp2(fmaf(z[e], c, -base));
+    sum.add(z, c2);
   }
-  const float wm = wave_max(ref);
+  const float wm = wave_max(sum.m);
   if (lane == 0) red_m[wave] = wm;
   __syncthreads();
   float M = red_m[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) M = fmaxf(M, red_m[w]);
-  s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - M));
+  const float s = wave_sum(in_unit(sum.m, sum.s, half_unit(M), c2));
   if (lane == 0) red_s[wave] = s;
   __syncthreads();
   if (threadIdx.x == 0) ms[blockIdx.x] = make_float2(M, red_s[0] + red_s[1] + red_s[2] + red_s[3]);
@@ -763,11 +798,11 @@ __global__ __launch_bounds__(kNT) void distill_row_kernel(const void *logits, in
   const double z = e.v >= 0 ? (double)ldf((const T *)logits + row * ld + e.v) : -INFINITY;
   const NamedSums n = named_sums<kWaves>(e, z, inv_temp, red);
   if (threadIdx.x >= 64) return;
-  const RowSums r = row_sums(e, n, ms + row * parts, parts);
+  const RowSums r = row_sums(e, n, ms + row * parts, parts, inv_temp);
   if (threadIdx.x == 0) {
     loss[row] = (float)r.loss;
-    lse[row] = (float)r.all;
-    lse[rows + row] = (float)r.rest;
+    lse[row] = as_float(r.all);
+    lse[rows + row] = as_float(r.rest);
   }
 }
 
@@ -791,6 +826,58 @@ __global__ __launch_bounds__(1024) void distill_stats_kernel(const float *loss, 
 // d logits of one part of a row.  A value that the list does not name gets
 // exp(z' - lse_rest) F with F = w (mass q_rest - rest), q_rest = exp(lse_rest - lse) (tail
 // 1), or exp(z' - lse) w mass (tail 0); a named one w (mass q - p).
+// A log-sum-exp l in float32 is off by 2^-24 |l|, and q by that much relatively.  From kFarLse
+// on (2^-10) the row is summed again, by the workgroup of its first part alone, which then
+// writes all of it (d logits may be the logits).
+constexpr float kFarLse = 16384.f;
+AJ_DEV bool far_lse(float l) { return fabsf(l) >= kFarLse && fabsf(l) <= FLT_MAX; }
+AJ_DEV LogSum near_lse(float l) { return l == -INFINITY ? LogSum{0.0, -INFINITY} : LogSum{l, 0.0}; }
+
+template <typename T, typename G>
+AJ_DEV void far_row_grad(const Row<T> &x, int vocab, const Teacher &t, int64_t row, const Listed &e, double zn,
+                         double inv_temp, G *out, uint32_t *bits, double *red, float2 *sums, RowGrad *shared) {
+  constexpr int R = kRun<T>;
+  const float c2 = (float)(2.0 * inv_temp * kLog2eD);
+  RunSum sum;
+  for (int u0 = 0; u0 < x.end; u0 += kSplit) {
+    const int u1 = min(u0 + kSplit, x.end);
+    __syncthreads();
+    for (int i = threadIdx.x; i < kSplit / 32; i += kNT) bits[i] = 0;
+    __syncthreads();
+    mark(bits, e.v, x.shift, vocab, u0, u1);
+    __syncthreads();
+#pragma unroll 1
+    for (int u = u0 + threadIdx.x * R; u < u1; u += kNT * R) {
+      float z[R];
+      Row<T>::values(x.load(u), z);
+      const uint32_t w = bits[(u - u0) >> 5] >> ((u - u0) & 31);
+#pragma unroll
+      for (int j = 0; j < R; ++j) z[j] = w >> j & 1 ? -INFINITY : z[j];
+      sum.add(z, c2);
+    }
+  }
+  const float wm = wave_max(sum.m);
+  const float s = wave_sum(in_unit(sum.m, sum.s, half_unit(wm), c2));
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = make_float2(wm, s);
+  const NamedSums n = named_sums<kWaves>(e, zn, inv_temp, red);
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const RowSums r = row_sums(e, n, sums, kWaves, inv_temp);
+    if (threadIdx.x == 0) shared->init(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, r.all, r.rest);
+  }
+  __syncthreads();
+  const RowGrad grad = *shared;
+#pragma unroll 1
+  for (int u = threadIdx.x * R; u < x.end; u += kNT * R) {
+    float z[R];
+    Row<T>::values(x.load(u), z);
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      if (u + j >= x.shift && u + j < x.end) stf(out + u + j, grad.other(z[j]));
+  }
+  __syncthreads();
+  if (e.v >= 0) stf(out + e.v + x.shift, grad.named(e, zn, inv_temp));
+}
 template <typename T, typename G>
 __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, int64_t ld, int vocab,
                                                           int rows, int parts, int width, Teacher t,
@@ -806,16 +893,25 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
   auto fetch = [&](int u) __attribute__((always_inline)) { x.load(b, u, threadIdx.x * R, kNT * R, kStep); };
   fetch(u0);
   const Listed e = listed<kWaves>(t, row, vocab, nullptr, ids, red);
-  const double all = lse[row], others = lse[rows + row];
+  const float all = lse[row], others = lse[rows + row];
   __shared__ RowGrad shared_grad;
-  if (threadIdx.x == 0) shared_grad.init(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, all, others);
+  G *out = dz + row * ldd - x.shift;
+  if (far_lse(all) || (t.tail && far_lse(others))) {
+    __shared__ uint32_t bits[kSplit / 32];
+    __shared__ float2 sums[kWaves];
+    if (u0 == 0)
+      far_row_grad<T, G>(x, vocab, t, row, e, e.v >= 0 ? (double)ldf((const T *)logits + row * ld + e.v) : -INFINITY,
+                         inv_temp, out, bits, red, sums, &shared_grad);
+    return;
+  }
+  if (threadIdx.x == 0)
+    shared_grad.init(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, near_lse(all), near_lse(others));
   __syncthreads();
   const RowGrad grad = shared_grad;
   // this part's named values, read before any is written (d logits may be the logits)
   const bool mine = e.v >= 0 && e.v + x.shift >= u0 && e.v + x.shift < u1;
   const float named = mine ? grad.named(e, ldf((const T *)logits + row * ld + e.v), inv_temp) : 0.f;
   __syncthreads();
-  G *out = dz + row * ldd - x.shift;
   // runs are stored whole where d logits is aligned as the runs are
   const bool vec = runs_aligned<G, R>(out);
   for (int u = u0; u < u1; u += kStep) {
@@ -878,15 +974,15 @@ __global__ __launch_bounds__(S::NT) void distill_step_kernel(const void *logits,
   __shared__ NamedSums shared_named;
   const int64_t row = blockIdx.x;
   const Row<T> x(logits, row, ld, vocab);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, me = threadIdx.x * R;
+  const int me = threadIdx.x * R;
   const int stripes = (x.end + C - 1) / C;
   typedef typename Row<T>::Bits Bits;
   auto fetch = [&](int k) __attribute__((always_inline)) { return x.whole(k * C + me); };
   Bits b[NR];
+  // (of a long row the last two wait until the list's sums in 64 bits have left registers)
+  constexpr int kEarly = kHoldLds ? NR - 2 : NR;
 #pragma unroll
-  for (int k = 0; k < NR; ++k) b[k] = fetch(k);
-  const int rim = threadIdx.x < 2 * R ? x.rim(threadIdx.x) : -1;
-  const float zr = rim >= 0 ? ldf(x.aligned + rim) : -INFINITY;
+  for (int k = 0; k < kEarly; ++k) b[k] = fetch(k);
   for (int i = threadIdx.x; i <= x.end / 32; i += kStepNT) bits[i] = 0;
   int my_v;
   float my_z;
@@ -902,7 +998,13 @@ __global__ __launch_bounds__(S::NT) void distill_step_kernel(const void *logits,
       shared_named = n;
     }
   }
-  float ref = -INFINITY, s = 0.f;
+  const int rim = threadIdx.x < 2 * R ? x.rim(threadIdx.x) : -1;
+  const float zr = rim >= 0 ? ldf(x.aligned + rim) : -INFINITY;
+  RunSum sum;
+  // copies of `me` that the compiler does not see into, or it keeps every run's place from the
+  // loads for the sums and the stores, for which there are no registers
+  int mine = me;
+  asm volatile("" : "+v"(mine));
   // adds the values of N runs, at stripes k0, k0 + 1 and so on, that are not named
   auto absorb = [&](auto N, const Bits *v, int k0) __attribute__((always_inline)) {
     constexpr int n = decltype(N)::value;
@@ -911,7 +1013,7 @@ __global__ __launch_bounds__(S::NT) void distill_step_kernel(const void *logits,
     for (int q = 0; q < n; ++q) {
       float f[R];
       Row<T>::values(v[q], f);
-      const int u = min((k0 + q) * C + me, x.end);
+      const int u = min((k0 + q) * C + mine, x.end);
       const uint32_t w = bits[u >> 5] >> (u & 31) & ((1u << R) - 1);
 #pragma unroll
       for (int j = 0; j < R; ++j) z[q * R + j] = f[j];
@@ -920,14 +1022,7 @@ __global__ __launch_bounds__(S::NT) void distill_step_kernel(const void *logits,
         for (int j = 0; j < R; ++j) z[q * R + j] = w >> j & 1 ? -INFINITY : f[j];
       }
     }
-    float m = z[0];
-#pragma unroll
-    for (int i = 1; i < n * R; ++i) m = fmaxf(m, z[i]);
-    const float up = fmaxf(ref, m * (float)(inv_temp * kLog2eD)), base = up == -INFINITY ? 0.f : up;
-    s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
-    ref = up;
-#pragma unroll
-    for (int i = 0; i < n * R; ++i) s += fast_exp2(fmaf(z[i], (float)(inv_temp * kLog2eD), -base));
+    sum.add(z, (float)(2.0 * inv_temp * kLog2eD));
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;
@@ -939,6 +1034,8 @@ __global__ __launch_bounds__(S::NT) void distill_step_kernel(const void *logits,
       absorb(One{}, v + 1, k + 1);
     }
   };
+#pragma unroll
+  for (int k = kEarly; k < NR; ++k) b[k] = fetch(k);
   // LDS's share by way of registers, two stripes ahead
 #pragma unroll
   for (int k = 0; k < kHoldLds; ++k) {
@@ -962,33 +1059,31 @@ __global__ __launch_bounds__(S::NT) void distill_step_kernel(const void *logits,
   }
   const bool rim_named = rim >= 0 && (bits[rim >> 5] >> (rim & 31) & 1);
   if (rim >= 0 && !rim_named) {
-    const float up = fmaxf(ref, zr * (float)(inv_temp * kLog2eD)), base = up == -INFINITY ? 0.f : up;
-    s *= ref == -INFINITY ? (s == s ? 0.f : s) : fast_exp2(ref - base);
-    ref = up;
-    s += fast_exp2(fmaf(zr, (float)(inv_temp * kLog2eD), -base));
+    const float z[1] = {zr};
+    sum.add(z, (float)(2.0 * inv_temp * kLog2eD));
   }
-  const float wm = wave_max(ref);
-  s = wave_sum(ref == -INFINITY ? s : s * fast_exp2(ref - wm));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float wm = wave_max(sum.m);
+  const float s = wave_sum(in_unit(sum.m, sum.s, half_unit(wm), (float)(2.0 * inv_temp * kLog2eD)));
   if (lane == 0) sums[wave] = make_float2(wm, s);
   lds_barrier();
   if (wave == 0) {
     const Listed e = shared_list;     // (of the first thread, whose mass and rest are the row's)
-    const RowSums r = row_sums(e, shared_named, sums, kStepWaves);
-    // the gradient from the rounded log-sum-exps, as the backward by itself has them
-    const float all = (float)r.all, rest = (float)r.rest;
+    const RowSums r = row_sums(e, shared_named, sums, kStepWaves, inv_temp);
     if (lane == 0) {
-      shared_grad.init(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, all, rest);
+      shared_grad.init(t, e, inv_temp, t.weight ? t.weight[row] : 1.f, r.all, r.rest);
       loss[row] = (float)r.loss;
-      lse[row] = all;
-      lse[rows + row] = rest;
+      lse[row] = as_float(r.all);
+      lse[rows + row] = as_float(r.rest);
     }
   }
   lds_barrier();
   const RowGrad grad = shared_grad;
   G *out = dz + row * ldd - x.shift;
   const bool vec = runs_aligned<G, R>(out);
+  asm volatile("" : "+v"(mine));
   auto put = [&](const Bits &v, int k) __attribute__((always_inline)) {
-    const int u = k * C + me;
+    const int u = k * C + mine;
     if (u < x.shift || u + R > x.end) return;
     float g[R];
     Row<T>::values(v, g);
@@ -1107,7 +1202,7 @@ void launch_loss(const aj_logits &lg, const aj_teacher &t, float *loss, float *l
                  int32_t *err, float2 *ms, hipStream_t st) {
   const Split s = row_split(lg.rows, lg.vocab);
   distill_part_kernel<T><<<(unsigned)lg.rows * s.parts, kNT, 0, st>>>(
-      lg.logits, lg.ld, lg.vocab, s.parts, s.width, teacher_of(t), lg.inv_temp * kLog2e, ms);
+      lg.logits, lg.ld, lg.vocab, s.parts, s.width, teacher_of(t), 2.f * lg.inv_temp * kLog2e, ms);
   distill_row_kernel<T><<<lg.rows, kNT, 0, st>>>(lg.logits, lg.ld, lg.vocab, lg.rows, s.parts, teacher_of(t),
                                                  lg.inv_temp, ms, loss, lse, err);
   if (stats) distill_stats_kernel<<<1, 1024, 0, st>>>(loss, t.weight, lg.rows, t.coef, stats);
