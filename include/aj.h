@@ -512,7 +512,8 @@ typedef struct {
  *   idx [rows, k] int32, logprob [rows, k] = logit * inv_temp - lse,
  *   lse [rows] = log sum exp(logit * inv_temp) over the whole row (natural log).
  * Logits of -inf have log-prob -inf (also where a row holds nothing else); a NaN or +inf
- * makes its row's lse NaN.  ws: aj_topk_workspace_bytes for at least these rows. */
+ * makes its row's lse NaN.  ws: aj_topk_workspace_bytes for at least these rows (0, here and
+ * in the queries below, for a k that the calls refuse). */
 size_t aj_topk_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
 int aj_topk_logprob(const aj_logits *lg, int32_t k, int32_t *idx, float *logprob, float *lse,
                     void *ws, size_t ws_bytes, void *stream);

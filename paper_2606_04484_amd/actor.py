@@ -335,6 +335,8 @@ class ActorUpdate:
 
     def _head_buffers(self, L, k):
         """Workspace of the LM head's calls on rows of logits, for the largest pack of L."""
+        if not 1 <= k <= 256:
+            raise C.AjError(f"lists of {k} tokens a target (1..256)")
         self._buffers(max((p["t1"] - p["t0"] for p in L.packs), default=0), 0)
         n = max((p["r1"] - p["r0"] for p in L.packs), default=0)
         need = C.aj_lm_head_workspace_bytes(self.lcfg, n, k)

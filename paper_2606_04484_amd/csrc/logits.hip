@@ -1259,7 +1259,7 @@ int check_grad(const aj_logits *lg, const void *dz, int64_t ldd, int d_dtype, co
 }  // namespace
 
 extern "C" size_t aj_topk_workspace_bytes(int32_t rows, int32_t vocab, int32_t k) {
-  if (rows < 0 || vocab <= 0 || k <= 0) return 0;
+  if (rows < 0 || vocab <= 0 || k <= 0 || k > kMaxK) return 0;
   return carve_top(rows, vocab, k, nullptr).bytes;
 }
 
@@ -1279,7 +1279,7 @@ extern "C" int aj_topk_logprob(const aj_logits *lg, int32_t k, int32_t *idx, flo
 }
 
 extern "C" size_t aj_distill_workspace_bytes(int32_t rows, int32_t vocab, int32_t k) {
-  if (rows < 0 || vocab <= 0 || k <= 0) return 0;
+  if (rows < 0 || vocab <= 0 || k <= 0 || k > kMaxK) return 0;
   return distill_ws(rows, vocab);
 }
 

@@ -860,7 +860,7 @@ int head_distill(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, cons
 }  // namespace
 
 extern "C" size_t aj_lm_head_workspace_bytes(const aj_loss_cfg *cfg, int32_t n_tgt, int32_t k) {
-  if (!cfg || n_tgt < 0 || k <= 0 || cfg->vocab <= 0 || cfg->d_model <= 0) return 0;
+  if (!cfg || n_tgt < 0 || k <= 0 || k > 256 || cfg->vocab <= 0 || cfg->d_model <= 0) return 0;
   return carve_head(*cfg, n_tgt, k, nullptr).bytes;
 }
 
