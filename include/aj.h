@@ -244,7 +244,7 @@ typedef struct {
  * (bit-identical on every call).  qkv, out, lse, d out and d qkv must not overlap.
  * ws: at least aj_attention_workspace_bytes(cfg, n_tok), for either direction; it
  * carries nothing from one to the other.
- * Errors as the block's; n_tok at most 2^30, n_tok * n_q_heads below 2^32.  Infinities and
+ * Errors as the block's; n_tok at most 2^30 - 1024, n_tok * n_q_heads below 2^32.  Infinities and
  * NaN in a row, or in its d out, reach with a window only what depends on that row by the
  * formulas; without one as in the block.
  */

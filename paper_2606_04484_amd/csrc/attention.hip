@@ -307,17 +307,18 @@ __global__ __launch_bounds__(256) void attn_fwd_f32_kernel(WinAttnArgs a) {
 // delta[h][row] = sum_d dO * O
 template <typename T>
 __global__ __launch_bounds__(256) void attn_delta_kernel(WinAttnBwdArgs a) {
-  const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (idx >= (int64_t)a.n_tok * a.Hq) return;
-  const int row = (int)(idx / a.Hq), h = (int)(idx % a.Hq);
-  const T *o = (const T *)a.o + (int64_t)row * a.Hq * a.hd + h * a.hd;
-  const T *d = (const T *)a.dout + (int64_t)row * a.Hq * a.hd + h * a.hd;
-  float s = 0.f;
-  for (int c = lane; c < a.hd; c += 64) s += ldf(o + c) * ldf(d + c);
+  for (int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); idx < (int64_t)a.n_tok * a.Hq;
+       idx += (int64_t)gridDim.x * 4) {
+    const int row = (int)(idx / a.Hq), h = (int)(idx % a.Hq);
+    const T *o = (const T *)a.o + (int64_t)row * a.Hq * a.hd + h * a.hd;
+    const T *d = (const T *)a.dout + (int64_t)row * a.Hq * a.hd + h * a.hd;
+    float s = 0.f;
+    for (int c = lane; c < a.hd; c += 64) s += ldf(o + c) * ldf(d + c);
 #pragma unroll
-  for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);
-  if (lane == 0) a.delta[(int64_t)h * a.n_tok + row] = s;
+    for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);
+    if (lane == 0) a.delta[(int64_t)h * a.n_tok + row] = s;
+  }
 }
 
 // dQ rows: dq = scale * sum_j P_j (dO.V_j - delta) K_j
@@ -509,33 +510,36 @@ template <typename T>
 __global__ __launch_bounds__(256) void attn_far_sums_kernel(WinAttnBwdArgs a, int chunk, float scale) {
   const int group = a.Hq / a.Hkv, w4 = a.hd / 2;   // 2 hd features of a key and KV head, in fours
   const int per = (a.n_sink * a.Hkv * w4 + 63) / 64;
-  const int start = blockIdx.x / per;   // the segment that starts in this run of `chunk` rows
-  const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, start * chunk + chunk - 1);
-  const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
-  if (s0 < 0 || s0 / chunk != start) return;
-  const int n_far = far_sinks(a, s1 - s0, chunk);
-  if (n_far == 0) return;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int idx = blockIdx.x % per * 64 + lane;
-  const int col = idx % w4 * 4, g = idx / w4 % a.Hkv, j = idx / w4 / a.Hkv;
-  const int n = (s1 - s0 + chunk - 1) / chunk * group;   // (chunk, head of the group)
   __shared__ f32x4_t red[4][64];
-  f32x4_t v{0.f, 0.f, 0.f, 0.f};
-  if (j < n_far) {
-    const float *p = a.sink_part + ((int64_t)2 * start * a.Hq * a.n_sink + j) * (2 * a.hd) + col;
+  for (int64_t item = blockIdx.x; item < (int64_t)(a.n_tok / chunk + 1) * per; item += gridDim.x) {
+    const int start = (int)(item / per);   // the segment that starts in this run of `chunk` rows
+    const int seg = seg_of(a.cu_seqlens, a.n_seg, a.base, start * chunk + chunk - 1);
+    const int s0 = a.cu_seqlens[seg] - a.base, s1 = min(a.cu_seqlens[seg + 1] - a.base, a.n_tok);
+    if (s0 < 0 || s0 / chunk != start) continue;
+    const int n_far = far_sinks(a, s1 - s0, chunk);
+    if (n_far == 0) continue;
+    const int idx = (int)(item % per) * 64 + lane;
+    const int col = idx % w4 * 4, g = idx / w4 % a.Hkv, j = idx / w4 / a.Hkv;
+    const int n = (s1 - s0 + chunk - 1) / chunk * group;   // (chunk, head of the group)
+    f32x4_t v{0.f, 0.f, 0.f, 0.f};
+    if (j < n_far) {
+      const float *p = a.sink_part + ((int64_t)2 * start * a.Hq * a.n_sink + j) * (2 * a.hd) + col;
 #pragma unroll 8
-    for (int i = w; i < n; i += 4)
-      v += *(const f32x4_t *)(p + ((int64_t)(i / group) * a.Hq + g * group + i % group) * a.n_sink * (2 * a.hd));
-  }
-  red[w][lane] = v;
-  __syncthreads();
-  if (w > 0 || j >= n_far) return;
-  v = red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane];
-  const bool is_k = col < a.hd;
-  T *out = (T *)a.dqkv + (int64_t)(s0 + j) * (a.Hq + 2 * a.Hkv) * a.hd + (a.Hq + (is_k ? g : a.Hkv + g)) * a.hd +
-           (is_k ? col : col - a.hd);
+      for (int i = w; i < n; i += 4)
+        v += *(const f32x4_t *)(p + ((int64_t)(i / group) * a.Hq + g * group + i % group) * a.n_sink * (2 * a.hd));
+    }
+    __syncthreads();   // the item before has been read
+    red[w][lane] = v;
+    __syncthreads();
+    if (w > 0 || j >= n_far) continue;
+    v = red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane];
+    const bool is_k = col < a.hd;
+    T *out = (T *)a.dqkv + (int64_t)(s0 + j) * (a.Hq + 2 * a.Hkv) * a.hd + (a.Hq + (is_k ? g : a.Hkv + g)) * a.hd +
+             (is_k ? col : col - a.hd);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) stf(out + e, is_k ? v[e] * scale : v[e]);
+    for (int e = 0; e < 4; ++e) stf(out + e, is_k ? v[e] * scale : v[e]);
+  }
 }
 
 // 16-feature chunks of a head, rounded up to an instantiated count
@@ -558,7 +562,7 @@ size_t attn_sink_floats(int window, int n_sink, int n_tok, int heads, int hd, in
 
 template <typename T>
 void attn_far_sums(const WinAttnBwdArgs &a, int chunk, hipStream_t s) {
-  const unsigned blocks = (unsigned)(a.n_tok / chunk + 1) * ((a.n_sink * a.Hkv * (a.hd / 2) + 63) / 64);
+  const unsigned blocks = launch_blocks((int64_t)(a.n_tok / chunk + 1) * ((a.n_sink * a.Hkv * (a.hd / 2) + 63) / 64));
   // the matrix-core pass leaves dK unscaled
   attn_far_sums_kernel<T><<<blocks, 256, 0, s>>>(a, chunk, chunk == kSinkChunk ? a.scale : 1.f);
 }
@@ -597,7 +601,7 @@ int attn_bwd(const WinAttnBwdArgs &args, hipStream_t s) {
     return fail(AJ_ERR_UNSUPPORTED, "attention backward: d out / d qkv not 16-byte aligned");
   const int64_t nd = (int64_t)a.n_tok * a.Hq;
   const int tk = timing_begin(s, AJ_KC_ATTN_BWD, 0.0);
-  attn_delta_kernel<T><<<(unsigned)((nd + 3) / 4), 256, 0, s>>>(a);
+  attn_delta_kernel<T><<<launch_blocks((nd + 3) / 4), 256, 0, s>>>(a);
   const int blocks = (a.n_tok + kRows - 1) / kRows;
   if (win) {
     AJ_NC_DISPATCH(a.hd, (attn_dq_f32_kernel<T, NC, true><<<dim3(blocks, a.Hq), 256, 0, s>>>(a)));
@@ -668,9 +672,9 @@ int check_attn(const aj_attn_cfg *c, const aj_varlen *v, const char *name) {
   AJ_REQUIRE(c->scale >= 0.f && c->scale <= 3e38f, AJ_ERR_SHAPE, "%s: scale", name);
   AJ_REQUIRE(v->n_tok >= 0 && v->n_seg >= 0 && (v->n_tok == 0 || v->n_seg > 0), AJ_ERR_SHAPE,
              "%s: n_tok %d n_seg %d", name, v->n_tok, v->n_seg);
-  // rows are added to in 32 bits, and waves of one (row, head) counted in them
-  AJ_REQUIRE(v->n_tok <= 1 << 30 && (int64_t)v->n_tok * c->n_q_heads < (int64_t)1 << 32,
-             AJ_ERR_SHAPE, "%s: n_tok %d (at most 2^30) times %d heads (below 2^32)", name, v->n_tok,
+  // a launch takes fewer than 2^32 threads along each of its sides, 4 n_tok + 1024 at most here
+  AJ_REQUIRE(v->n_tok <= (1 << 30) - 1024 && (int64_t)v->n_tok * c->n_q_heads < (int64_t)1 << 32,
+             AJ_ERR_SHAPE, "%s: n_tok %d (at most 2^30 - 1024) times %d heads (below 2^32)", name, v->n_tok,
              c->n_q_heads);
   AJ_REQUIRE(v->n_tok == 0 || v->cu_seqlens, AJ_ERR_NULL, "%s: null offsets", name);
   return AJ_OK;

@@ -1465,19 +1465,20 @@ __global__ __launch_bounds__(256, 1) void attn_sinks_mfma_kernel(WinAttnBwdArgs 
 }
 
 __global__ __launch_bounds__(256) void attn_delta_bf16_kernel(WinAttnBwdArgs a) {
-  const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (idx >= (int64_t)a.n_tok * a.Hq) return;
-  const int row = (int)(idx / a.Hq), h = (int)(idx % a.Hq);
-  const bf16_t *o = (const bf16_t *)a.o + (int64_t)row * a.Hq * a.hd + h * a.hd;
-  const bf16_t *d = (const bf16_t *)a.dout + (int64_t)row * a.Hq * a.hd + h * a.hd;
-  float s = 0.f;
-  for (int c = lane; c < a.hd; c += 64) s += bf2f(o[c]) * bf2f(d[c]);
+  for (int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); idx < (int64_t)a.n_tok * a.Hq;
+       idx += (int64_t)gridDim.x * 4) {
+    const int row = (int)(idx / a.Hq), h = (int)(idx % a.Hq);
+    const bf16_t *o = (const bf16_t *)a.o + (int64_t)row * a.Hq * a.hd + h * a.hd;
+    const bf16_t *d = (const bf16_t *)a.dout + (int64_t)row * a.Hq * a.hd + h * a.hd;
+    float s = 0.f;
+    for (int c = lane; c < a.hd; c += 64) s += bf2f(o[c]) * bf2f(d[c]);
 #pragma unroll
-  for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);
-  // stored negated: the dK/dV and dQ passes start their dP accumulators from
-  // it, so that dP - delta costs no vector instruction
-  if (lane == 0) a.delta[(int64_t)h * a.n_tok + row] = -s;
+    for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);
+    // stored negated: the dK/dV and dQ passes start their dP accumulators from
+    // it, so that dP - delta costs no vector instruction
+    if (lane == 0) a.delta[(int64_t)h * a.n_tok + row] = -s;
+  }
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
@@ -1616,7 +1617,7 @@ int attn_bwd_mfma(const WinAttnBwdArgs &a, hipStream_t s) {
   const int64_t nd = (int64_t)a.n_tok * a.Hq;
   const int tk = timing_begin(s, AJ_KC_ATTN_BWD, 0.0);
   if (!a.few && !windowed(a.window, a.n_tok))   // (the windowed dQ pass forms delta itself)
-    attn_delta_bf16_kernel<<<(unsigned)((nd + 3) / 4), 256, 0, s>>>(a);
+    attn_delta_bf16_kernel<<<launch_blocks((nd + 3) / 4), 256, 0, s>>>(a);
   if (a.hd == 128) launch_bwd<128>(a, s);
   else launch_bwd<64>(a, s);
   timing_end(s, tk);

@@ -99,6 +99,10 @@ inline size_t gemm_partial_floats(int64_t M, int64_t N, bool f32) {
 int gemm_f32_pieces(int M, int N, int K, size_t partial_cap);
 
 // ---------------------------------------------------------------- attention
+// Workgroups of 256 threads for n items whose kernel strides over them: a launch takes
+// fewer than 2^32 threads.
+inline unsigned launch_blocks(int64_t n) { return (unsigned)(n < (1 << 23) ? n : 1 << 23); }
+
 struct AttnArgs {
   int n_tok, n_seg, Hq, Hkv, hd;
   int base;             // cu_seqlens values are row offsets + base
