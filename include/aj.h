@@ -500,7 +500,7 @@ int aj_logprob_pg_loss_bwd(const aj_loss_cfg *cfg, const aj_loss_in *in, const v
  * nothing but -inf.
  */
 typedef struct {
-  int32_t rows, vocab;          /* vocab at most 2^24 */
+  int32_t rows, vocab;          /* vocab at most 2^24, rows * ceil((vocab + 7) / 65536) below 2^24 */
   int64_t ld;                   /* elements from row to row, >= vocab; rows need no alignment */
   int32_t dtype;                /* aj_dtype of the logits */
   float inv_temp;               /* probabilities are softmax(logits * inv_temp); > 0 */

@@ -1152,6 +1152,7 @@ TopWs carve_top(int rows, int vocab, int k, void *base) {
 }
 
 struct Split { int parts, width; };
+int whole_parts(int vocab) { return (vocab + 7 + kSplit - 1) / kSplit; }    // the fewest a row is cut into
 // Parts of a row: kSplit values at most, fewer until 2048 workgroups run, 2048 at least.
 Split row_split(int rows, int vocab) {
   int width = kSplit;
@@ -1167,8 +1168,9 @@ int check_logits(const aj_logits *lg, const char *name) {
              "%s: rows %d vocab %d (at most 2^24) ld %lld", name, lg->rows, lg->vocab, (long long)lg->ld);
   AJ_REQUIRE(lg->inv_temp > 0.f && lg->inv_temp <= 1e30f, AJ_ERR_SHAPE, "%s: inv_temp %g", name,
              (double)lg->inv_temp);
-  AJ_REQUIRE((int64_t)lg->rows * (lg->vocab / 2048 + 2) < (int64_t)1 << 31, AJ_ERR_SHAPE,
-             "%s: rows %d of vocab %d", name, lg->rows, lg->vocab);
+  // workgroups of 256 threads, of which a launch takes fewer than 2^32
+  AJ_REQUIRE((int64_t)lg->rows * whole_parts(lg->vocab) < 1 << 24, AJ_ERR_SHAPE,
+             "%s: rows %d of %d parts each (below 2^24 in all)", name, lg->rows, whole_parts(lg->vocab));
   AJ_REQUIRE(lg->rows == 0 || lg->logits, AJ_ERR_NULL, "%s: null logits", name);
   AJ_REQUIRE(((uintptr_t)lg->logits & (lg->dtype == AJ_BF16 ? 1 : 3)) == 0, AJ_ERR_SHAPE,
              "%s: logits between elements", name);
@@ -1225,7 +1227,8 @@ void launch_grad(const aj_logits &lg, const aj_teacher &t, const float *lse, voi
 // are cut into parts.
 constexpr int kStepRows = 512, kStepLeast = 32768;
 bool one_step(const aj_logits &lg) {
-  return lg.vocab <= kSmallVocab || (lg.rows >= kStepRows && lg.vocab >= kStepLeast && lg.vocab <= kStepVocab);
+  return lg.vocab <= kSmallVocab || (lg.rows >= kStepRows && lg.rows < 1 << 22 && lg.vocab >= kStepLeast &&
+                                     lg.vocab <= kStepVocab);     // (2^22 workgroups of 1024 threads: too many)
 }
 template <typename T, typename G>
 void launch_step(const aj_logits &lg, const aj_teacher &t, float *loss, float *lse, int32_t *err, void *dz,

@@ -22,3 +22,19 @@ def test_workspace_of_a_list_too_long(rows, k):
 def test_workspace_of_the_longest_list(rows, vocab):
     assert capi.aj_topk_workspace_bytes(rows, vocab, 256) >= capi.aj_topk_workspace_bytes(rows, vocab, 1) > 0
     assert capi.aj_distill_workspace_bytes(rows, vocab, 256) > 0
+
+
+P16 = C.c_void_p(16)
+
+
+@pytest.mark.parametrize("rows, vocab", [(1 << 24, 1), ((1 << 24) - 1, 65530), (1 << 16, 1 << 24), ((1 << 31) - 1, 100)])
+def test_rows_past_a_launch(rows, vocab):
+    """Rows for which a launch has not threads enough are refused before any work."""
+    L = capi.lib()
+    lg = C.byref(capi.Logits(rows, vocab, vocab, 0, 1.0, P16))
+    t = C.byref(capi.Teacher(1, 1, P16, P16, None, 1.0))
+    big = 1 << 60
+    assert L.aj_topk_logprob(lg, 1, P16, P16, P16, P16, big, None) == 2
+    assert L.aj_distill_loss_fwd(lg, t, P16, P16, None, None, P16, big, None) == 2
+    assert L.aj_distill_loss_bwd(lg, t, P16, P16, vocab, 0, None) == 2
+    assert L.aj_distill_loss_fwd_bwd(lg, t, P16, P16, None, None, P16, vocab, 0, P16, big, None) == 2
