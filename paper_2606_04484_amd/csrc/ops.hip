@@ -296,8 +296,8 @@ __global__ void scale_cast_kernel(const float *in, int64_t n, float scale, T *ou
 }
 
 __global__ void fill_kernel(float *p, int64_t n, float v) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < n) p[i] = v;
+  const int64_t stride = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) p[i] = v;
 }
 
 inline unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
@@ -424,7 +424,7 @@ void transpose16(const void *src, int rows, int cols, void *dst, hipStream_t s) 
 }
 
 void fill_f32(float *p, int64_t n, float v, hipStream_t s) {
-  if (n > 0) fill_kernel<<<blocks_for(n, 256), 256, 0, s>>>(p, n, v);
+  if (n > 0) fill_kernel<<<launch_blocks((n + 255) / 256), 256, 0, s>>>(p, n, v);
 }
 
 #define AJ_INST(T)                                                                              \

@@ -68,3 +68,32 @@ def test_rows_of_logits():
         torch.cuda.synchronize()
         assert bool(((loss - kl).abs() <= 2e-6).all())
         assert bool(((dz - (want.exp() - p)).abs() <= 2e-6).all())
+
+
+def test_hidden_gradient_past_a_launch():
+    """d h of 2^32 elements and more is cleared to its end."""
+    from paper_2606_04484_amd import capi
+    D, V, n, dev = 8192, 64, (1 << 19) + 3, "cuda"
+    cfg = capi.LossCfg(D, V, 1 << 14, 0.2, 1e-6, capi.AJ_BF16, 0)
+    h = torch.zeros(n, D, dtype=torch.bfloat16, device=dev)
+    rows = torch.tensor([5, n - 1], device=dev)
+    h[rows] = torch.randn(2, D, device=dev).bfloat16()
+    w = (torch.randn(V, D, device=dev) * 0.02).bfloat16()
+    gamma = torch.ones(D, dtype=torch.bfloat16, device=dev)
+    t = capi.teacher(torch.tensor([[1, 7], [9, 2]], dtype=torch.int32, device=dev),
+                     torch.tensor([[-1.0, -2.0], [-0.5, -3.0]], device=dev), tail=True)
+    ws = torch.empty(capi.aj_lm_head_workspace_bytes(cfg, 2, 2), dtype=torch.uint8, device=dev)
+
+    def run(h, rows):
+        dh = torch.full(h.shape, 7.0, device=dev)
+        capi.aj_lm_head_distill(cfg, (rows + 1).to(torch.int32), h, gamma, w, 1.0, t, torch.empty(2, device=dev), dh,
+                                None, None, ws)
+        torch.cuda.synchronize()
+        return dh
+
+    dh = run(h, rows)
+    few = run(h[rows].contiguous(), torch.arange(2, device=dev))
+    assert torch.equal(dh[rows], few) and bool(few.any())
+    dh[rows] = 0
+    for a in range(0, n, 1 << 16):
+        assert not bool(dh[a:a + (1 << 16)].any())
