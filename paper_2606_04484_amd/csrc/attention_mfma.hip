@@ -941,6 +941,14 @@ struct DkvSched {
   }
 };
 
+// One past the last query that key kv meets in the pass of a window.
+AJ_DEV int keys_end(const WinAttnBwdArgs &a, int kv) {
+  const int end = seg_end(a, kv);
+  if (end - kv <= a.window) return end;
+  const int s0 = seg_start(a, kv);
+  return kv - s0 >= a.n_sink ? kv + a.window : kv - s0 < far_sinks(a, end - s0, kSinkChunk) ? kv : end;
+}
+
 template <int HD, int NW, bool WIN>
 __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a, int parts) {
   using TT = TokTile<HD, NW>;
@@ -966,14 +974,7 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
   const int k0 = kt * 32 * NW;
   const int kv = k0 + 32 * w + lq;            // the key row this lane owns
   const bool kvv = kv < a.n_tok;
-  int ke = kvv ? seg_end(a, kv) : 0;          // queries of the key: [kv, ke)
-  if constexpr (WIN) {
-    if (kvv && ke - kv > a.window) {
-      const int s0 = seg_start(a, kv);
-      if (kv - s0 >= a.n_sink) ke = kv + a.window;
-      else if (kv - s0 < far_sinks(a, ke - s0, kSinkChunk)) ke = kv;
-    }
-  }
+  const int ke = !kvv ? 0 : WIN ? keys_end(a, kv) : seg_end(a, kv);   // queries of the key: [kv, ke)
   const bf16_t *qkv = (const bf16_t *)a.qkv;
   const bf16_t *dout = (const bf16_t *)a.dout;
   if constexpr (WIN) {
@@ -1259,19 +1260,28 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_mfma_kernel(WinAttnBwdArgs a
   }
   if constexpr (WIN) {
     if (__builtin_amdgcn_ballot_w64(kvv && (nonfinite(dk) | nonfinite(dv)))) {
-      const int half = opaque(hl);
+      // everything of the lane's again, operands too: kept for here, it takes registers from the
+      // main loop (40 at head_dim 64, and with them the second wave of a SIMD)
+      const int tid = opaque(threadIdx.x), half = tid >> 5 & 1, first = k0 + (tid >> 6) * 32;
+      const int key = first + (tid & 31), row = min(key, a.n_tok - 1);
+      const int end = key < a.n_tok ? keys_end(a, key) : 0, q1 = wave_max(end);
+      const bf16_t *krow = qkv + (int64_t)row * ld + (a.Hq + g) * HD + 8 * half, *vrow = krow + a.Hkv * HD;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        kf[kk] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(krow + 16 * kk));
+        vf[kk] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t *)(vrow + 16 * kk));
+      }
       clear(dk);
       clear(dv);
-      const int q1 = wave_max(ke);
 #pragma unroll 1
       for (int h = h0; h < h0 + n_h; ++h)
 #pragma unroll 1
-        for (int q = k0 + 32 * w; q < q1; ++q) {
+        for (int q = first; q < q1; ++q) {
           const bf16_t *qrow = qkv + (int64_t)q * ld + h * HD, *drow = dout + (int64_t)q * ldo + h * HD;
           const int64_t at = (int64_t)h * a.n_tok + q;
           const float p = fast_exp2(fmaf(row_dot<HD>(qrow, kf, half), c, -a.lse[at]));
           const float ds = p * (row_dot<HD>(drow, vf, half) + a.delta[at]);
-          const bool in = kvv & (q >= kv) & (q < ke);
+          const bool in = (q >= key) & (q < end);
           row_add<HD>(dv, drow, p, in, half);
           row_add<HD>(dk, qrow, ds, in, half);
         }
