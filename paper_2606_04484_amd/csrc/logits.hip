@@ -949,10 +949,14 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
 struct LongRows {
   static constexpr int NT = 1024, REG = 12, REG16 = 8, LDS = 8, WORDS = 6144;    // 128 KB of runs, 24 KB of bits
 };
+// of more than kLongVocab values, whose bits take a run's place in LDS
+struct VeryLongRows {
+  static constexpr int NT = 1024, REG = 12, REG16 = 8, LDS = 7, WORDS = 8448;
+};
 struct ShortRows {
   static constexpr int NT = 256, REG = 12, REG16 = 8, LDS = 0, WORDS = 512;
 };
-constexpr int kStepVocab = LongRows::WORDS * 32 - 16;
+constexpr int kLongVocab = LongRows::WORDS * 32 - 16, kStepVocab = VeryLongRows::WORDS * 32 - 16;
 constexpr int kSmallVocab = ShortRows::NT * ShortRows::REG * 4 - 8;
 static_assert(kSmallVocab <= ShortRows::WORDS * 32 - 16 && kSmallVocab <= ShortRows::NT * ShortRows::REG16 * 8 - 8,
               "short rows fit");
@@ -1235,6 +1239,9 @@ void launch_step(const aj_logits &lg, const aj_teacher &t, float *loss, float *l
                  int64_t ldd, hipStream_t st) {
   if (lg.vocab <= kSmallVocab)
     distill_step_kernel<T, G, ShortRows><<<lg.rows, ShortRows::NT, 0, st>>>(
+        lg.logits, lg.ld, lg.vocab, lg.rows, teacher_of(t), lg.inv_temp, loss, lse, err, (G *)dz, ldd);
+  else if (lg.vocab > kLongVocab)
+    distill_step_kernel<T, G, VeryLongRows><<<lg.rows, VeryLongRows::NT, 0, st>>>(
         lg.logits, lg.ld, lg.vocab, lg.rows, teacher_of(t), lg.inv_temp, loss, lse, err, (G *)dz, ldd);
   else
     distill_step_kernel<T, G, LongRows><<<lg.rows, LongRows::NT, 0, st>>>(
