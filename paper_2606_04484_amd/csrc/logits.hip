@@ -941,10 +941,9 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
 }
 
 // Loss and gradient of a row in one go: one workgroup of 16 waves per row keeps what it
-// reads for the loss on the chip, in registers (kHoldReg runs a thread) and LDS
-// (kHoldLds), and forms the gradient from there; of a float32 row of 152064 values that
-// is 62 %, the rest is read again, newest first, while the caches still have it, and a
-// bfloat16 row of that length is kept whole.
+// reads for the loss on the chip, in registers (REG runs a thread) and LDS (LDS runs), and
+// forms the gradient from there; of a row of 152064 values that is 81920 in float32 (54 %) and
+// 131072 in bfloat16 (86 %), the rest is read again, newest first, while the caches still have it.
 // Rows of up to kSmallVocab values take four waves each, which hold all of a row in registers.
 struct LongRows {
   static constexpr int NT = 1024, REG = 12, REG16 = 8, LDS = 8, WORDS = 6144;    // 128 KB of runs, 24 KB of bits
@@ -1227,11 +1226,21 @@ void launch_grad(const aj_logits &lg, const aj_teacher &t, const float *lse, voi
                                                        teacher_of(t), lg.inv_temp, lse, (float *)dz, ldd);
 }
 
-// Long rows take a workgroup each from this many rows (two rounds of the CUs) and values on; fewer
-// are cut into parts.
-constexpr int kStepRows = 512, kStepLeast = 32768;
+// Long rows take a workgroup each from two rounds of the CUs on, and from so many values that
+// what they keep is worth the list's sums at the start of every row; others go by the loss's and
+// the gradient's kernels, cut into parts.  Those two / the one, us, k 64, bfloat16 d logits:
+//   rows of 152064   256 rows   384       512       1024      4096
+//     float32         68 / 52    94 / 89  139 / 107 317 / 226 1177 / 866
+//     bfloat16        49 / 42    66 / 72   85 / 78  182 / 159  738 / 628
+//   4096 rows of    32768       40000     50257     65536     80000     100000
+//     float32       286 / 327  344 / 358 465 / 400 594 / 443 680 / 503 824 / 583
+//     bfloat16      166 / 338  215 / 350 299 / 375 397 / 400 446 / 433 543 / 481
+// (At 256 rows, one full round, the one kernel is the faster too; at 128, 42 / 40, they are
+// alike, and at 64, 28 / 37, it is the slower.)
+constexpr int kStepRows = 512, kStepLeastF32 = 45056, kStepLeastBf16 = 73728;
 bool one_step(const aj_logits &lg) {
-  return lg.vocab <= kSmallVocab || (lg.rows >= kStepRows && lg.rows < 1 << 22 && lg.vocab >= kStepLeast &&
+  const int least = lg.dtype == AJ_BF16 ? kStepLeastBf16 : kStepLeastF32;
+  return lg.vocab <= kSmallVocab || (lg.rows >= kStepRows && lg.rows < 1 << 22 && lg.vocab >= least &&
                                      lg.vocab <= kStepVocab);     // (2^22 workgroups of 1024 threads: too many)
 }
 template <typename T, typename G>

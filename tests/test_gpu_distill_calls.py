@@ -3,6 +3,7 @@ they refuse, beyond ordinary batches."""
 import pytest
 import torch
 
+from test_gpu_distill import test_many_long_rows as many_long_rows
 from tests.gpu_cases import Case, workload
 from workloads import get_config
 
@@ -24,3 +25,13 @@ def test_lists_of_a_length_that_is_refused(k):
         A.distill_step(L, idx, idx.float())
     torch.cuda.synchronize()
     assert all(not bool(g.any()) for g in A.G.values())
+
+
+@pytest.mark.parametrize("tail", [False, True], ids=["listed", "tail"])
+@pytest.mark.parametrize("dtype, grad", [("f32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("vocab, k, pad, offset", [(45056, 30, 0, 0), (73728, 9, 5, 3), (196592, 16, 0, 0),
+                                                   (196593, 64, 1, 0), (262144, 33, 3, 5), (270320, 8, 0, 0),
+                                                   (270321, 5, 0, 1)])
+def test_ends_of_the_ranges_of_long_rows(vocab, k, pad, offset, dtype, grad, tail):
+    """A workgroup's share of a row, at the sizes where the ways of forming its gradient change."""
+    many_long_rows(vocab, k, pad, offset, dtype, grad, tail)

@@ -117,7 +117,7 @@ def check(got, want, grad):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("what", WHAT + ["listed alone", "unlisted alone"])
 @pytest.mark.parametrize("rows, vocab, k, pad, offset", [(5, 2003, 20, 0, 1), (6, 70001, 100, 3, 0),
-                                                        (515, 33001, 33, 0, 2)])
+                                                        (515, 75001, 33, 0, 2)])
 def test_distill(rows, vocab, k, pad, offset, what, dtype, part, tail):
     few = min(rows, 9)
     z = rows_of(what, few, vocab, dtype, seed=rows)
