@@ -536,7 +536,9 @@ typedef struct {
 /* With q = softmax(logits * inv_temp), q_rest the sum of q over the tokens that are not
  * listed and p_rest = max(0, 1 - sum p) (tail 1; 0 for tail 0):
  *   loss[row] = sum_k p_k (log p_k - log q_k) + p_rest (log p_rest - log q_rest)
- * (0 for a row with nothing listed; not scaled by weight or coef).  lse: [2, rows], the
+ * (0 for a row with nothing listed; not scaled by weight or coef).  Where q_rest is 0, the
+ * whole vocabulary listed or all else at -inf, a p_rest of at most 2^-14 is the rounding of
+ * the log-probs and counts as 0; a larger one makes the loss infinite.  lse: [2, rows], the
  * log-sum-exp of the row's logits * inv_temp and that of the tokens not listed; the
  * backward reads it, and sums a row again where one it needs is 16384 or more (float32
  * would be off by 2^-10 and more).  stats (may be NULL): float32[2] accumulated: [0] the sum of

@@ -659,10 +659,22 @@ AJ_DEV NamedSums named_sums(const Listed &e, double z, double inv_temp, double *
   return {log_of(m, sz, inv_temp), block_sum<WAVES>(term, red)};
 }
 
+// What a teacher's float32 log-probs leave of 1 by their rounding, at most: half a step each, and
+// the error of the log-sum-exp they share (some 600 of 2^-24).
+constexpr double kListRounding = 1.0 / 16384;
+// Where the student has nothing outside the list, that much there is no class of the teacher's:
+// its divergence would be infinite or not as the roundings fall.
+AJ_DEV void settle(Listed &e, const LogSum &rest) {
+  if (rest.none() && e.rest <= kListRounding) {
+    e.mass -= e.rest;
+    e.rest = 0.0;
+  }
+}
+
 // A row's log-sum-exps, of all values and of those not named, and its loss; in one wave.
 // ms: the sums of the values not named, with their units.
 struct RowSums { LogSum all, rest; double loss; };
-AJ_DEV RowSums row_sums(const Listed &e, const NamedSums &n, const float2 *ms, int parts, double inv_temp) {
+AJ_DEV RowSums row_sums(Listed e, const NamedSums &n, const float2 *ms, int parts, double inv_temp) {
   const int lane = threadIdx.x & 63;
   RowSums r;
   float M = -INFINITY;
@@ -672,6 +684,7 @@ AJ_DEV RowSums row_sums(const Listed &e, const NamedSums &n, const float2 *ms, i
   for (int q = lane; q < parts; q += 64) s += part_in_unit(ms[q], M, inv_temp * kLog2eD);
   r.rest = log_of(M, wave_sum(s), inv_temp);
   r.all = join(r.rest, n.list);
+  settle(e, r.rest);
   r.loss = n.term;
   const double p = e.mass - e.rest;
   if (p != 0.0) r.loss += p * ((r.all.unit - n.list.unit) + r.all.log);
@@ -683,11 +696,13 @@ AJ_DEV RowSums row_sums(const Listed &e, const NamedSums &n, const float2 *ms, i
 struct RowGrad {
   float c2, half, more, f;
   int none;       // nothing listed: no loss, no gradient, whatever the logits
-  double w;
+  double w, mass;
   LogSum all;
-  AJ_DEV void init(const Teacher &t, const Listed &e, double inv_temp, double weight, const LogSum &all_,
+  AJ_DEV void init(const Teacher &t, Listed e, double inv_temp, double weight, const LogSum &all_,
                    const LogSum &rest) {
+    settle(e, rest);
     all = all_;
+    mass = e.mass;
     w = (double)t.coef * inv_temp * weight;
     const LogSum &l = t.tail ? rest : all;
     half = l.none() ? 0.f : (float)(0.5 * l.unit / inv_temp);
@@ -699,8 +714,8 @@ struct RowGrad {
   AJ_DEV float other(float z) const {
     return none ? 0.f : fast_exp2(fmaf(fmaf(z, 0.5f, -half), c2, -more)) * f;
   }
-  AJ_DEV float named(const Listed &e, double z, double inv_temp) const {
-    return none ? 0.f : (float)(w * (e.mass * exp((z * inv_temp - all.unit) - all.log) - e.p));
+  AJ_DEV float named(double p, double z, double inv_temp) const {
+    return none ? 0.f : (float)(w * (mass * exp((z * inv_temp - all.unit) - all.log) - p));
   }
 };
 
@@ -876,7 +891,7 @@ AJ_DEV void far_row_grad(const Row<T> &x, int vocab, const Teacher &t, int64_t r
       if (u + j >= x.shift && u + j < x.end) stf(out + u + j, grad.other(z[j]));
   }
   __syncthreads();
-  if (e.v >= 0) stf(out + e.v + x.shift, grad.named(e, zn, inv_temp));
+  if (e.v >= 0) stf(out + e.v + x.shift, grad.named(e.p, zn, inv_temp));
 }
 template <typename T, typename G>
 __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, int64_t ld, int vocab,
@@ -910,7 +925,7 @@ __global__ __launch_bounds__(kNT) void distill_bwd_kernel(const void *logits, in
   const RowGrad grad = shared_grad;
   // this part's named values, read before any is written (d logits may be the logits)
   const bool mine = e.v >= 0 && e.v + x.shift >= u0 && e.v + x.shift < u1;
-  const float named = mine ? grad.named(e, ldf((const T *)logits + row * ld + e.v), inv_temp) : 0.f;
+  const float named = mine ? grad.named(e.p, ldf((const T *)logits + row * ld + e.v), inv_temp) : 0.f;
   __syncthreads();
   // runs are stored whole where d logits is aligned as the runs are
   const bool vec = runs_aligned<G, R>(out);
@@ -1119,11 +1134,7 @@ __global__ __launch_bounds__(S::NT) void distill_step_kernel(const void *logits,
   }
   if (rim >= 0) stf(out + rim, grad.other(zr));
   __syncthreads();    // the named ones over what the runs left there
-  if (my_v >= 0) {
-    Listed e = shared_list;
-    e.p = list_p[threadIdx.x];
-    stf(out + my_v + x.shift, grad.named(e, my_z, inv_temp));
-  }
+  if (my_v >= 0) stf(out + my_v + x.shift, shared_grad.named(list_p[threadIdx.x], my_z, inv_temp));
 }
 
 // ------------------------------------------------------------------ host

@@ -1,8 +1,11 @@
 """Calls of the teacher's and the student's operators that their documentation allows, or that
 they refuse, beyond ordinary batches."""
+import math
+
 import pytest
 import torch
 
+from test_gpu_distill import E, LSE, definition, distill, lists
 from test_gpu_distill import test_many_long_rows as many_long_rows
 from tests.gpu_cases import Case, workload
 from workloads import get_config
@@ -35,3 +38,33 @@ def test_lists_of_a_length_that_is_refused(k):
 def test_ends_of_the_ranges_of_long_rows(vocab, k, pad, offset, dtype, grad, tail):
     """A workgroup's share of a row, at the sizes where the ways of forming its gradient change."""
     many_long_rows(vocab, k, pad, offset, dtype, grad, tail)
+
+
+@pytest.mark.parametrize("part", ["step", "apart"])
+@pytest.mark.parametrize("vocab, masked", [(40, False), (256, False), (3000, True), (20000, True)])
+def test_a_list_of_all_that_the_student_can_say(vocab, masked, part):
+    """What rounding leaves of the teacher's 1 is no class of its own where the student has
+    nothing outside the list; a mass that is really missing there is."""
+    g = torch.Generator().manual_seed(vocab)
+    rows, k = 64, min(vocab, 200)
+    z = torch.randn(rows, vocab, generator=g)
+    if masked:
+        z[:, k:] = -math.inf
+    k = k if masked else vocab
+    lp = torch.log_softmax(torch.randn(rows, k, generator=g) * 2, 1)
+    idx = torch.stack([torch.randperm(k, generator=g) for _ in range(rows)]).to(torch.int32)
+    left = 1 - lp.double().exp().sum(1)
+    assert bool((left > 0).any()) and bool((left < 0).any()) and bool((left.abs() < 2 ** -14).all())
+    loss, _, dz, stats, _ = distill(z.cuda(), 1.0, idx, lp, True, None, 1.0, "f32", part=part)
+    want = definition(z, 1.0, idx, lp, False, torch.ones(rows).double())
+    # the lists' own sum is 1 to within 2^-14, no more is known of the teacher
+    assert bool(((loss - want[0]).abs() <= left.abs() * (2 + want[0]) + 3 * LSE + 8 * E * (40 + want[0])).all())
+    assert bool(((dz - want[2]).abs() <= (left.abs()[:, None] + LSE + 300 * E) * want[3] + 1e-30).all())
+    assert math.isfinite(float(stats[0]))
+    # a token that the teacher gives a mass, and neither the list nor the student holds
+    gone = idx[:, 3:4].long().clone()
+    z.scatter_(1, gone, -math.inf)
+    idx[:, 3] = -1
+    loss = distill(z.cuda(), 1.0, idx, lp, True, None, 1.0, "f32", part=part)[0]
+    missing = 1 - torch.where(idx >= 0, lp.double().exp(), 0.0).sum(1)
+    assert torch.equal(loss == math.inf, missing > 2 ** -14) and bool((missing > 2 ** -14).any())
