@@ -529,7 +529,8 @@ typedef struct {
                                    class, all tokens that are not listed */
   const int32_t *idx;           /* [rows, k] */
   const float *logprob;         /* [rows, k] natural log; -inf: probability 0 */
-  const float *weight;          /* [rows] weight of each row, or NULL for 1 */
+  const float *weight;          /* [rows] weight of each row, or NULL for 1; a row of weight 0 has no
+                                   gradient and no share of stats, whatever it holds */
   float coef;                   /* of every row's gradient and share of stats */
 } aj_teacher;
 

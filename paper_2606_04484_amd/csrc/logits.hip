@@ -695,7 +695,7 @@ AJ_DEV RowSums row_sums(Listed e, const NamedSums &n, const float2 *ms, int part
 // The gradient of the values not named, 2^((z - 2 half) c - more) f, and of a named one.
 struct RowGrad {
   float c2, half, more, f;
-  int none;       // nothing listed: no loss, no gradient, whatever the logits
+  int none;       // nothing listed, or a weight of 0: no gradient, whatever the logits
   double w, mass;
   LogSum all;
   AJ_DEV void init(const Teacher &t, Listed e, double inv_temp, double weight, const LogSum &all_,
@@ -709,7 +709,7 @@ struct RowGrad {
     more = l.none() ? 0.f : (float)((l.unit - 2.0 * half * inv_temp + l.log) * kLog2eD);
     c2 = (float)(2.0 * inv_temp * kLog2eD);
     f = (float)(t.tail ? w * (e.mass * exp(log_ratio(rest, all)) - e.rest) : w * e.mass);
-    none = e.mass == 0.0;
+    none = e.mass == 0.0 || weight == 0.0;
   }
   AJ_DEV float other(float z) const {
     return none ? 0.f : fast_exp2(fmaf(fmaf(z, 0.5f, -half), c2, -more)) * f;
@@ -826,7 +826,10 @@ __global__ __launch_bounds__(1024) void distill_stats_kernel(const float *loss, 
                                                              int rows, float coef, float *stats) {
   __shared__ double red[16];
   double s = 0.0;
-  for (int i = threadIdx.x; i < rows; i += 1024) s += (double)coef * (weight ? weight[i] : 1.f) * loss[i];
+  for (int i = threadIdx.x; i < rows; i += 1024) {
+    const float w = weight ? weight[i] : 1.f;
+    if (w != 0.f) s += (double)coef * w * loss[i];
+  }
   s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();

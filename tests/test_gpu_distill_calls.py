@@ -68,3 +68,27 @@ def test_a_list_of_all_that_the_student_can_say(vocab, masked, part):
     loss = distill(z.cuda(), 1.0, idx, lp, True, None, 1.0, "f32", part=part)[0]
     missing = 1 - torch.where(idx >= 0, lp.double().exp(), 0.0).sum(1)
     assert torch.equal(loss == math.inf, missing > 2 ** -14) and bool((missing > 2 ** -14).any())
+
+
+@pytest.mark.parametrize("part", ["step", "apart"])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, vocab", [(7, 2000), (6, 70001), (513, 90000)])
+def test_rows_of_weight_zero(rows, vocab, grad, part):
+    """A row of weight 0 may hold anything: no gradient, no share of the sum; the others' as ever."""
+    g = torch.Generator().manual_seed(rows)
+    few = min(rows, 7)
+    z = torch.randn(few, vocab, generator=g)
+    idx, lp = lists(z, 20, 3, 1.0)
+    w = torch.rand(few, generator=g) + 0.5
+    w[1::2] = 0
+    bad, blp = z.clone(), lp.clone()
+    bad[1], bad[3, 5], bad[5, ::2] = math.nan, math.inf, -math.inf
+    blp[1, 2] = blp[3] = math.nan
+    if few > 5:
+        blp[5, 0] = math.inf
+    at = torch.arange(rows) % few
+    a = distill(z[at].cuda(), 1.0, idx[at], lp[at], True, w[at], 0.5, grad, part=part)
+    b = distill(bad[at].cuda(), 1.0, idx[at], blp[at], True, w[at], 0.5, grad, part=part)
+    on = w[at] > 0
+    assert bool((b[2][~on] == 0).all()) and torch.equal(a[2], b[2])
+    assert torch.equal(a[0][on], b[0][on]) and torch.equal(a[3], b[3])
