@@ -570,9 +570,11 @@ int aj_distill_loss_fwd_bwd(const aj_logits *lg, const aj_teacher *t, float *los
  * ascend, each once.
  * err: AJ_DEVERR_OFFSETS for a target outside the pack (for _distill also for one that
  * is not above the one before: of two in one row dh keeps either), and the lists' errors.
- * ws: aj_lm_head_workspace_bytes(cfg, n_tgt, k): the logits of a slab (4 bytes each; with
- * bfloat16 2 more for d logits) and 134 MB at most for split reductions. */
+ * ws: aj_lm_head_workspace_bytes(cfg, n_tgt, k) for either: the logits of a slab (4 bytes
+ * each; with bfloat16 2 more for d logits) and 134 MB at most for split reductions; _topk
+ * alone takes aj_lm_head_topk_workspace_bytes, without what the gradients need. */
 size_t aj_lm_head_workspace_bytes(const aj_loss_cfg *cfg, int32_t n_tgt, int32_t k);
+size_t aj_lm_head_topk_workspace_bytes(const aj_loss_cfg *cfg, int32_t n_tgt, int32_t k);
 int aj_lm_head_topk(const aj_loss_cfg *cfg, const aj_loss_in *in, const void *h,
                     const void *final_norm, const void *w_vocab, float inv_temp, int32_t k,
                     int32_t *idx, float *logprob, float *lse, int32_t *err, void *ws,

@@ -333,13 +333,13 @@ class ActorUpdate:
                                 cu, pos, max_len, x, self.ckpt, self.saved, dh, dh,
                                 self.layer_grads, self.bws, base=t0)
 
-    def _head_buffers(self, L, k):
+    def _head_buffers(self, L, k, query):
         """Workspace of the LM head's calls on rows of logits, for the largest pack of L."""
         if not 1 <= k <= 256:
             raise C.AjError(f"lists of {k} tokens a target (1..256)")
         self._buffers(max((p["t1"] - p["t0"] for p in L.packs), default=0), 0)
         n = max((p["r1"] - p["r0"] for p in L.packs), default=0)
-        need = C.aj_lm_head_workspace_bytes(self.lcfg, n, k)
+        need = query(self.lcfg, n, k)
         if getattr(self, "hws", None) is None or self.hws.numel() < need:
             self.hws = torch.empty(max(need, 1), dtype=torch.uint8, device=self.dev)
 
@@ -347,7 +347,7 @@ class ActorUpdate:
         """What a student learns from this policy on layout L: the k most probable tokens at
         every target, (idx int32, logprob float32) [n_mask, k], under softmax(logits /
         temperature).  Forward only."""
-        self._head_buffers(L, k)
+        self._head_buffers(L, k, C.aj_lm_head_topk_workspace_bytes)
         self.refresh_transposed()
         idx = torch.empty(L.n_mask, k, dtype=torch.int32, device=self.dev)
         logprob = torch.empty(L.n_mask, k, dtype=torch.float32, device=self.dev)
@@ -375,7 +375,7 @@ class ActorUpdate:
                             f"{L.n_mask} targets")
         if weight is not None and tuple(weight.shape) != (L.n_mask,):
             raise C.AjError(f"distill_step: weight {tuple(weight.shape)} for {L.n_mask} targets")
-        self._head_buffers(L, idx.shape[1])
+        self._head_buffers(L, idx.shape[1], C.aj_lm_head_workspace_bytes)
         if coef is None:
             coef = 1.0 / L.n_mask if L.n_mask else 0.0
         W, G = self.W, self.G

@@ -177,6 +177,7 @@ EXPORTS = {
     "aj_distill_loss_fwd_bwd": (C.c_int, [C.POINTER(Logits), C.POINTER(Teacher), vp, vp, vp, vp,
                                           vp, i64, i32, vp, sz, vp]),
     "aj_lm_head_workspace_bytes": (sz, [C.POINTER(LossCfg), i32, i32]),
+    "aj_lm_head_topk_workspace_bytes": (sz, [C.POINTER(LossCfg), i32, i32]),
     "aj_lm_head_topk": (C.c_int, [C.POINTER(LossCfg), C.POINTER(LossIn), vp, vp, vp, f32, i32, vp,
                                   vp, vp, vp, vp, sz, vp]),
     "aj_lm_head_distill": (C.c_int, [C.POINTER(LossCfg), C.POINTER(LossIn), vp, vp, vp, f32,
@@ -668,6 +669,11 @@ def aj_distill_loss_fwd_bwd(logits, inv_temp, t, loss, lse, dlogits, ws, stats=N
 
 def aj_lm_head_workspace_bytes(cfg, n_tgt, k):
     return int(lib().aj_lm_head_workspace_bytes(C.byref(cfg), int(n_tgt), int(k)))
+
+
+def aj_lm_head_topk_workspace_bytes(cfg, n_tgt, k):
+    """What aj_lm_head_topk alone takes."""
+    return int(lib().aj_lm_head_topk_workspace_bytes(C.byref(cfg), int(n_tgt), int(k)))
 
 
 def _head(name, cfg, targets, h, final_norm, w_vocab, row_base, w_vocab_t):

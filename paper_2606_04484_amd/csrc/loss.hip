@@ -737,16 +737,23 @@ struct HeadWs {
   int32_t *tpos, *trow;
 };
 
-HeadWs carve_head(const aj_loss_cfg &c, int n_tgt, int k, void *base) {
+// (the teacher's calls need none of what the student's gradients go through)
+HeadWs carve_head(const aj_loss_cfg &c, int n_tgt, int k, bool student, void *base) {
   const bool f32 = c.dtype != AJ_BF16;
   const int slab = std::min(n_tgt, kHeadSlab);
   aj::Carver cv(base);
-  HeadWs w;
+  HeadWs w{};
   w.hn = cv.take<char>((int64_t)n_tgt * c.d_model * (f32 ? 4 : 2));
   w.rstd = cv.take<float>(n_tgt);
   w.tpos = cv.take<int32_t>(n_tgt);
   w.trow = cv.take<int32_t>(n_tgt);
   w.z = cv.take<float>((int64_t)slab * c.vocab);
+  if (!student) {
+    w.rows_ws_bytes = aj_topk_workspace_bytes(slab, c.vocab, k);
+    w.rows_ws = cv.take<char>(w.rows_ws_bytes);
+    w.bytes = cv.bytes();
+    return w;
+  }
   // float32: d logits over the logits
   w.dz = f32 ? (void *)w.z : cv.take<char>((int64_t)slab * c.vocab * 2);
   w.lse = cv.take<float>(2 * (int64_t)slab);
@@ -755,7 +762,7 @@ HeadWs carve_head(const aj_loss_cfg &c, int n_tgt, int k, void *base) {
   w.splitk_floats = std::max(aj::gemm_partial_floats(c.vocab, c.d_model, f32),
                              aj::gemm_partial_floats(slab, c.d_model, f32));
   w.splitk = cv.take<float>(w.splitk_floats);
-  w.rows_ws_bytes = std::max(aj_topk_workspace_bytes(slab, c.vocab, k), aj_distill_workspace_bytes(slab, c.vocab, k));
+  w.rows_ws_bytes = aj_distill_workspace_bytes(slab, c.vocab, k);
   w.rows_ws = cv.take<char>(w.rows_ws_bytes);
   w.bytes = cv.bytes();
   return w;
@@ -861,7 +868,13 @@ int head_distill(const aj_loss_cfg &c, const aj_loss_in &in, const void *h, cons
 
 extern "C" size_t aj_lm_head_workspace_bytes(const aj_loss_cfg *cfg, int32_t n_tgt, int32_t k) {
   if (!cfg || n_tgt < 0 || k <= 0 || k > 256 || cfg->vocab <= 0 || cfg->d_model <= 0) return 0;
-  return carve_head(*cfg, n_tgt, k, nullptr).bytes;
+  // both calls' (the distillation's is not always the larger: small vocabularies, long lists)
+  return std::max(carve_head(*cfg, n_tgt, k, true, nullptr).bytes, carve_head(*cfg, n_tgt, k, false, nullptr).bytes);
+}
+
+extern "C" size_t aj_lm_head_topk_workspace_bytes(const aj_loss_cfg *cfg, int32_t n_tgt, int32_t k) {
+  if (!cfg || n_tgt < 0 || k <= 0 || k > 256 || cfg->vocab <= 0 || cfg->d_model <= 0) return 0;
+  return carve_head(*cfg, n_tgt, k, false, nullptr).bytes;
 }
 
 extern "C" int aj_lm_head_topk(const aj_loss_cfg *cfg, const aj_loss_in *in, const void *h, const void *final_norm,
@@ -873,7 +886,7 @@ extern "C" int aj_lm_head_topk(const aj_loss_cfg *cfg, const aj_loss_in *in, con
   AJ_REQUIRE(k <= cfg->vocab, AJ_ERR_SHAPE, "%s: k %d of vocab %d", name, k, cfg->vocab);
   if (in->n_tgt == 0) return AJ_OK;
   AJ_REQUIRE(h && final_norm && w_vocab && idx && logprob && lse && ws, AJ_ERR_NULL, "%s: null pointer", name);
-  const HeadWs w = carve_head(*cfg, in->n_tgt, k, ws);
+  const HeadWs w = carve_head(*cfg, in->n_tgt, k, false, ws);
   AJ_REQUIRE(ws_bytes >= w.bytes, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes, w.bytes);
   hipStream_t st = (hipStream_t)stream;
   const aj::StageSpan span(st, AJ_KC_STAGE_LOSS);
@@ -894,7 +907,7 @@ extern "C" int aj_lm_head_distill(const aj_loss_cfg *cfg, const aj_loss_in *in, 
   AJ_REQUIRE(dh, AJ_ERR_NULL, "%s: null dh", name);
   AJ_REQUIRE(in->n_tgt == 0 || (h && final_norm && w_vocab && loss && ws && t->idx && t->logprob), AJ_ERR_NULL,
              "%s: null pointer", name);
-  const HeadWs w = carve_head(*cfg, in->n_tgt, t->k, ws);
+  const HeadWs w = carve_head(*cfg, in->n_tgt, t->k, true, ws);
   AJ_REQUIRE(in->n_tgt == 0 || ws_bytes >= w.bytes, AJ_ERR_WORKSPACE, "%s: workspace %zu < %zu", name, ws_bytes,
              w.bytes);
   hipStream_t st = (hipStream_t)stream;

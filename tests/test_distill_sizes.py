@@ -38,3 +38,20 @@ def test_rows_past_a_launch(rows, vocab):
     assert L.aj_distill_loss_fwd(lg, t, P16, P16, None, None, P16, big, None) == 2
     assert L.aj_distill_loss_bwd(lg, t, P16, P16, vocab, 0, None) == 2
     assert L.aj_distill_loss_fwd_bwd(lg, t, P16, P16, None, None, P16, vocab, 0, P16, big, None) == 2
+
+
+@pytest.mark.parametrize("d, v, dtype", [(64, 72, 0), (1536, 151936, 1), (3584, 152064, 1), (128, 1024, 0), (64, 8, 1)])
+def test_workspace_of_the_teacher_alone(d, v, dtype):
+    """Less than the student's, and as that one enough for fewer targets."""
+    cfg = capi.LossCfg(d, v, 1 << 14, 0.2, 1e-6, dtype, 0)
+    for k in (1, 8, min(v, 256)):
+        sizes = [capi.aj_lm_head_topk_workspace_bytes(cfg, n, k) for n in range(1, 9000, 7)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
+        both = [capi.aj_lm_head_workspace_bytes(cfg, n, k) for n in range(1, 9000, 7)]
+        assert both == sorted(both) and all(a <= b for a, b in zip(sizes, both))
+    for n in (1, 8192, 20000):
+        teacher, student = (q(cfg, n, 8) for q in (capi.aj_lm_head_topk_workspace_bytes,
+                                                   capi.aj_lm_head_workspace_bytes))
+        # no d hidden, and with bfloat16 no d logits
+        assert student - teacher >= 4 * n * d + (2 * min(n, 8192) * v if dtype else 0) - (1 << 20)
+    assert capi.aj_lm_head_topk_workspace_bytes(cfg, 4, 257) == 0

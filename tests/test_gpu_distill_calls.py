@@ -7,6 +7,7 @@ import torch
 
 from test_gpu_distill import E, LSE, definition, distill, lists
 from test_gpu_distill import test_many_long_rows as many_long_rows
+from test_gpu_distill_head import BASE, setup
 from tests.gpu_cases import Case, workload
 from workloads import get_config
 
@@ -92,3 +93,22 @@ def test_rows_of_weight_zero(rows, vocab, grad, part):
     on = w[at] > 0
     assert bool((b[2][~on] == 0).all()) and torch.equal(a[2], b[2])
     assert torch.equal(a[0][on], b[0][on]) and torch.equal(a[3], b[3])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n_tok, n_tgt", [(5, 3), (900, 700), (8600, 8400)])
+def test_the_teacher_stays_in_its_workspace(n_tok, n_tgt, dtype):
+    from paper_2606_04484_amd import capi
+    cfg, h, gamma, w, rows, targets = setup(n_tok, n_tgt, dtype)
+    res = []
+    for query in (capi.aj_lm_head_topk_workspace_bytes, capi.aj_lm_head_workspace_bytes):
+        size = query(cfg, n_tgt, 11)
+        ws = torch.full((size + 4096,), 255, dtype=torch.uint8, device="cuda")
+        idx = torch.zeros(n_tgt, 11, dtype=torch.int32, device="cuda")
+        lp, lse = torch.zeros(n_tgt, 11, device="cuda"), torch.zeros(n_tgt, device="cuda")
+        capi.aj_lm_head_topk(cfg, targets.cuda(), h.cuda(), gamma.cuda(), w.cuda(), 1.0, idx, lp, lse, ws[:size],
+                             row_base=BASE)
+        torch.cuda.synchronize()
+        assert bool((ws[size:] == 255).all())
+        res.append((idx, lp, lse))
+    assert all(torch.equal(a, b) for a, b in zip(*res))
