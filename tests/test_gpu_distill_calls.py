@@ -7,7 +7,7 @@ import torch
 
 from test_gpu_distill import E, LSE, definition, distill, lists
 from test_gpu_distill import test_many_long_rows as many_long_rows
-from test_gpu_distill_head import BASE, setup
+from test_gpu_distill_head import BASE, D, setup
 from tests.gpu_cases import Case, workload
 from workloads import get_config
 
@@ -112,3 +112,58 @@ def test_the_teacher_stays_in_its_workspace(n_tok, n_tgt, dtype):
         assert bool((ws[size:] == 255).all())
         res.append((idx, lp, lse))
     assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+@pytest.mark.parametrize("vocab", [257, 1003])
+@pytest.mark.parametrize("n_tok, n_tgt", [(70, 33), (700, 600)])
+def test_head_of_an_odd_vocabulary_in_half_precision(n_tok, n_tgt, vocab):
+    """bfloat16 weights of a vocabulary that is no multiple of 8: loss, d h, d W and d gamma
+    against the definition on the same numbers, with what rounding the normalised rows and
+    d logits to bfloat16 allows."""
+    from paper_2606_04484_amd import capi
+    g = torch.Generator().manual_seed(vocab)
+    dt = torch.bfloat16
+    h = (torch.randn(n_tok, D, generator=g) * 2).to(dt)
+    gamma = (1 + 0.3 * torch.randn(D, generator=g)).to(dt)
+    W = (torch.randn(vocab, D, generator=g) * 0.4).to(dt)
+    rows = torch.randperm(n_tok, generator=g)[:n_tgt].sort().values
+    cfg = capi.LossCfg(D, vocab, 1 << 14, 0.2, 1e-6, capi.AJ_BF16, 0)
+    x, gm, w = h.double()[rows], gamma.double(), W.double()
+    r = (x.square().mean(1, keepdim=True) + 1e-6).rsqrt()
+    exact = x * r * gm
+    hn = exact.to(dt).double()            # a row is normalised in float32 and rounded once
+    idx, lp = lists((hn @ w.T).float(), 9, 3, 1.0)
+    loss, sw, dz, size = definition(hn @ w.T, 1.0, idx, lp, True, torch.ones(n_tgt))
+    t = capi.teacher(idx.cuda(), lp.cuda(), tail=True)
+    z = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    ws = torch.full((capi.aj_lm_head_workspace_bytes(cfg, n_tgt, 9),), 255, dtype=torch.uint8, device="cuda")
+    out, dh, dg, dw = z(n_tgt), z(n_tok, D).fill_(7.0), z(D), z(vocab, D)
+    capi.aj_lm_head_distill(cfg, (rows + 1 + BASE).to(torch.int32).cuda(), h.cuda(), gamma.cuda(), W.cuda(), 1.0, t, out,
+                            dh, dg, dw, ws, row_base=BASE)
+    torch.cuda.synchronize()
+    # a normalised value next to the middle of two of its type may be rounded the other way: a
+    # step of bfloat16, where its float32 value is within (D / 2 + 8) 2^-24 of the middle
+    a = E * (D / 2 + 8)
+    step = 2.0 ** (torch.floor(torch.log2(exact.abs())) - 7)
+    flip = torch.where((exact - hn).abs() + a * exact.abs() >= step / 2, step, 0.0)
+    assert float((flip > 0).double().mean()) < 0.01
+    b = (flip @ w.abs().T + E * (D + 4) * (hn.abs() @ w.abs().T)).amax(1, keepdim=True)
+    assert bool(((out.cpu() - loss).abs() <= 2.1 * b[:, 0] + 3 * LSE + 8 * E * (sw[0].abs() + loss.abs())).all())
+    u = 2.0 ** -8
+    ddz = (4.2 * b + LSE + 6 * E * (sw[0].abs()[:, None] + 40)) * size * 1.01 + 1e-37
+    ddz = ddz + u * (dz.abs() + ddz)                                # d logits are rounded
+    top = dz.abs() + ddz
+    want = dz.T @ hn
+    room = ddz.T @ (hn.abs() + flip) + dz.abs().T @ flip + E * (n_tgt + 8) * top.T @ hn.abs()
+    assert bool(((dw.cpu() - want).abs() <= room + E * want.abs()).all())
+    dhn, ddhn = dz @ w, ddz @ w.abs() + E * (vocab + 8) * top @ w.abs()
+    back = lambda v, s: r * v + s * x.abs() * r ** 3 / D * (v * x.abs()).sum(1, keepdim=True)  # noqa: E731
+    dx = r * gm * dhn - x * r ** 3 / D * (gm * dhn * x).sum(1, keepdim=True)
+    mag = gm.abs() * (dhn.abs() + ddhn)
+    assert bool(((dh.cpu()[rows] - dx).abs() <= back(gm.abs() * ddhn, 1) + E * (3 * D + 40) * back(mag, 1)).all())
+    wg = (dhn * x * r).sum(0)
+    room = (ddhn * x.abs() * r).sum(0) + E * (n_tgt + D + 24) * ((dhn.abs() + ddhn) * x.abs() * r).sum(0)
+    assert bool(((dg.cpu() - wg).abs() <= room).all())
+    rest = torch.ones(n_tok, dtype=torch.bool)
+    rest[rows] = False
+    assert bool((dh.cpu()[rest] == 0).all())
