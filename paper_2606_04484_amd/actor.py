@@ -370,7 +370,7 @@ class ActorUpdate:
         at the same temperature); tail: the rest of the vocabulary is one more class, else the
         lists are renormalised; weight: optional float32 [n_mask]; coef: default 1 / n_mask.
         Returns float32 [2]: the loss (sum of coef * weight * KL), targets."""
-        if tuple(idx.shape) != tuple(logprob.shape) or idx.shape[0] != L.n_mask:
+        if idx.dim() != 2 or tuple(idx.shape) != tuple(logprob.shape) or idx.shape[0] != L.n_mask:
             raise C.AjError(f"distill_step: lists {tuple(idx.shape)}, {tuple(logprob.shape)} for "
                             f"{L.n_mask} targets")
         if weight is not None and tuple(weight.shape) != (L.n_mask,):

@@ -694,6 +694,8 @@ def aj_lm_head_topk(cfg, targets, h, final_norm, w_vocab, inv_temp, idx, logprob
     float32 [n_tgt]; cfg: loss_cfg."""
     name = "aj_lm_head_topk"
     a = _head(name, cfg, targets, h, final_norm, w_vocab, row_base, w_vocab_t)
+    if not isinstance(idx, torch.Tensor) or idx.dim() != 2:
+        raise AjError(f"{name}: idx must be a matrix")
     n, k = a.n_tgt, idx.shape[1]
     _operands(name, {"idx": (idx, (torch.int32,), (n, k)), "logprob": (logprob, (torch.float32,), (n, k)),
                      "lse": (lse, (torch.float32,), (n,)),

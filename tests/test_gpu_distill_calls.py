@@ -167,3 +167,19 @@ def test_head_of_an_odd_vocabulary_in_half_precision(n_tok, n_tgt, vocab):
     rest = torch.ones(n_tok, dtype=torch.bool)
     rest[rows] = False
     assert bool((dh.cpu()[rest] == 0).all())
+
+
+def test_lists_that_are_no_matrix():
+    from paper_2606_04484_amd import actor, capi
+    cfg, h, gamma, w, rows, targets = setup(50, 20, torch.float32)
+    flat = torch.zeros(20, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    with pytest.raises(capi.AjError, match="idx must be a matrix"):
+        capi.aj_lm_head_topk(cfg, targets.cuda(), h.cuda(), gamma.cuda(), w.cuda(), 1.0, flat, flat.float(),
+                             flat.float(), ws, row_base=BASE)
+    case = Case(workload(get_config(0).model))
+    L = actor.merge(actor.upload_timelines(case.tl, case.old))
+    A = actor.ActorUpdate(case.m, case.device_weights())
+    flat = torch.zeros(L.n_mask, dtype=torch.int32, device="cuda")
+    with pytest.raises(capi.AjError, match="lists"):
+        A.distill_step(L, flat, flat.float())
