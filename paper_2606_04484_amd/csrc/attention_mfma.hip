@@ -628,11 +628,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_mfma_kernel(WinAttnArgs a
 }
 
 // ------------------------------------------------------------------ dQ
-// Key tiles of a workgroup up to which delta is formed exactly (128 rows with windows of
-// at most 64 keys, or of short segments).  dQ of 20000 tokens of 28 heads of 128, window 64:
-// 222 us without, 298 with; window 100, past the rule: 246, and the error of d qkv is 1.42 to
-// 1.45 times that of rounding it, of 8 keys without the pass 1.50, with it 1.41.
-constexpr int kFewTiles = 4;
+// Delta is formed exactly by workgroups that have at most kFewTiles key tiles and a row that sees
+// fewer than kFewKeys keys: a short window, or the start of a segment among or just before their
+// rows.  Forward and backward of 20000 tokens of 28 heads of 128, window 64: 670 us without, 746
+// with the pass in every workgroup of so few tiles.  Error of d q, in those of rounding it,
+// without / with: window 2 2.29 / 1.41, 4 1.80 / 1.41, 8 1.62 / 1.42, 16 1.53 / 1.42, 32 1.49 / 1.42,
+// 64 1.46 / 1.42; segments of 10 tokens 1.77 / 1.42, of 40 1.63 / 1.42, of 100 1.56 / 1.42.
+constexpr int kFewTiles = 4, kFewKeys = 33;
 
 // Same workgroup shape as the forward; a lane owns one query.
 template <int HD, int NW, bool WIN>
@@ -657,7 +659,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(WinAttnBwdArgs
   const bf16_t *dout = (const bf16_t *)a.dout;
   // the first key of the row's window
   const int low = WIN ? max(qs, q - a.window + 1) : qs;
-  if (threadIdx.x == 0) shared_tiles.init(a, q0, 32 * NW);
+  __shared__ int shared_early;    // whether a row sees few keys
+  if (threadIdx.x == 0) {
+    shared_tiles.init(a, q0, 32 * NW);
+    if (WIN && shared_tiles.n <= kFewTiles)
+      shared_early = a.window + a.n_sink < kFewKeys || q0 - shared_tiles.s0 < kFewKeys ||
+                     seg_start(a, shared_tiles.hi) > q0;
+  }
   bf16x8_t qf[KS], df[KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
@@ -728,7 +736,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_mfma_kernel(WinAttnBwdArgs
   // bfloat16, through dO . O, would be as large an error as the one of dS (15 tokens:
   // dQ and dK 1.7 times as far off as by that alone).  Where the keys are few, delta
   // is taken as the sum of p dP in a pass of its own over them.
-  if (WIN && kt.n <= kFewTiles) {
+  if (WIN && kt.n <= kFewTiles && __builtin_amdgcn_ballot_w64(shared_early)) {
     float sum = 0.f;
     spread(0.f);
     for (int it = 0; it < kt.n; ++it) {
