@@ -327,7 +327,13 @@ size_t aj_block_workspace_bytes(const aj_block_cfg *cfg, int32_t n_tok, int32_t 
  * AJ_ERR_WORKSPACE for a short workspace.
  * Infinities and NaN in a row reach the rows that attend to it; with bfloat16,
  * head_dim 64 or 128 and no window also other rows within the same tiles (64 keys, up to
- * 256 queries), whose masked weights are zeros in the same matrix products. */
+ * 256 queries), whose masked weights are zeros in the same matrix products.
+ * More than 128 sinks cost a window's backward what full attention of their queries does
+ * (from 129 on twice the time and more); aj_attention_bwd too.
+ * With bfloat16, head_dim 64 or 128 and no window the backward takes sum_j p_ij (do_i v_j) as
+ * do_i o_i of the rounded output for every row; aj_attention_bwd, on packs whose segments
+ * have at most 256 rows on average, and a window's backward sum it themselves for rows of
+ * few keys (d q of a row of 2 keys is 2.3 times as far off as its own rounding otherwise). */
 int aj_varlen_block_fwd(const aj_block_cfg *cfg, const aj_block_weights *w, const aj_varlen *vl,
                         const void *x, void *y, void *saved, void *ws, size_t ws_bytes,
                         void *stream);

@@ -682,9 +682,10 @@ int check_attn(const aj_attn_cfg *c, const aj_varlen *v, const char *name) {
 
 // Mean rows of a segment up to which a pack is one of early rows: most workgroups of the
 // windowed dQ then have few tiles.  Forward and backward, windowed kernels against causal
-// ones, us: 15 tokens of 12 heads of 128 36 / 39, 200 tokens 51 / 47, 900 in 9 segments 69 / 63;
-// 20000 of 28 heads in 500 segments 646 / 667, in 160 737 / 778 (of 64 457 / 455), in 80
-// 883 / 938 (of 64 559 / 571).
+// ones, us: 15 tokens of 12 heads of 128 33 / 35, 200 tokens 52 / 51, 900 in 9 segments 67 / 60;
+// 20000 of 28 heads of 128 in 500 segments 558 / 594, in 160 602 / 627, in 80 624 / 699 (of 64
+// 316 / 330, 355 / 358, 348 / 395).  Segments of no tokens count: four of 5000 among 100 of
+// them take the windowed kernels too, 3988 / 4001 us.
 constexpr int kFewRows = 256;
 
 float attn_scale(const aj_attn_cfg &c) {
