@@ -705,7 +705,8 @@ struct RowGrad {
     mass = e.mass;
     w = (double)t.coef * inv_temp * weight;
     const LogSum &l = t.tail ? rest : all;
-    half = l.none() ? 0.f : (float)(0.5 * l.unit / inv_temp);
+    // (a log-sum-exp over a tiny inv_temp may leave float32; `more` makes up for the bound)
+    half = l.none() ? 0.f : (float)min(max(0.5 * l.unit / inv_temp, -0.5 * FLT_MAX), 0.5 * FLT_MAX);
     more = l.none() ? 0.f : (float)((l.unit - 2.0 * half * inv_temp + l.log) * kLog2eD);
     c2 = (float)(2.0 * inv_temp * kLog2eD);
     f = (float)(t.tail ? w * (e.mass * exp(log_ratio(rest, all)) - e.rest) : w * e.mass);

@@ -152,3 +152,23 @@ def test_lowest_values_at_a_low_temperature(part, inv_temp):
     inv = float(torch.tensor(inv_temp, dtype=torch.float32))
     got = distill(z.cuda(), inv, idx, lp, True, None, 1.0, "f32", part=part)
     check(got, definition(z, inv, idx, lp, True, torch.ones(9).double()), "f32")
+
+
+@pytest.mark.parametrize("inv_temp", [1e-30, 1e-38, 1e-44])
+@pytest.mark.parametrize("what", ["random", "both ends"])
+@pytest.mark.parametrize("part", ["step", "apart"])
+def test_temperatures_at_which_all_tokens_are_alike(part, what, inv_temp):
+    z = rows_of(what, 7, 4000, "f32")
+    inv = float(torch.tensor(inv_temp, dtype=torch.float32))
+    at = place(z)[:, :20]
+    idx, lp, lse = topk(z, z.cuda(), 20, inv)
+    unit, log = log_sum(z.double(), inv, torch.ones_like(z, dtype=torch.bool))
+    assert torch.equal(idx.long(), at) and bool(((lse - unit - log).abs() <= LSE + 2 * E * lse.abs()).all())
+    lpw = (z.double().gather(1, at) * inv - unit[:, None]) - log[:, None]
+    assert bool(((lp - lpw).abs() <= LSE + 3 * E * lpw.abs()).all())
+    ti, tl = lists(torch.randn(7, 4000, generator=torch.Generator().manual_seed(7)), 20, 3, 1.0)
+    one = torch.ones(7).double()
+    got = distill(z.cuda(), inv, ti, tl, True, None, 1.0 / inv if inv > 1e-37 else 1e30, "f32", part=part)
+    want = definition(z, inv, ti, tl, True, one * (float(torch.tensor(1.0 / inv)) if inv > 1e-37 else
+                                                   float(torch.tensor(1e30))))
+    check(got, want, "f32")
