@@ -333,21 +333,22 @@ class ActorUpdate:
                                 cu, pos, max_len, x, self.ckpt, self.saved, dh, dh,
                                 self.layer_grads, self.bws, base=t0)
 
-    def _head_buffers(self, L, k, query):
-        """Workspace of the LM head's calls on rows of logits, for the largest pack of L."""
+    def _head_buffers(self, L, k, name, query):
+        """Workspace `name` of the LM head's calls on rows of logits, for the largest pack of L.
+        (One for the teacher's and one for the student's: neither call moves the other's.)"""
         if not 1 <= k <= 256:
             raise C.AjError(f"lists of {k} tokens a target (1..256)")
         self._buffers(max((p["t1"] - p["t0"] for p in L.packs), default=0), 0)
         n = max((p["r1"] - p["r0"] for p in L.packs), default=0)
-        need = query(self.lcfg, n, k)
-        if getattr(self, "hws", None) is None or self.hws.numel() < need:
-            self.hws = torch.empty(max(need, 1), dtype=torch.uint8, device=self.dev)
+        need, ws = query(self.lcfg, n, k), getattr(self, name, None)
+        if ws is None or ws.numel() < need:
+            setattr(self, name, torch.empty(max(need, 1), dtype=torch.uint8, device=self.dev))
 
     def teacher_topk(self, L, k, temperature=1.0):
         """What a student learns from this policy on layout L: the k most probable tokens at
         every target, (idx int32, logprob float32) [n_mask, k], under softmax(logits /
         temperature).  Forward only."""
-        self._head_buffers(L, k, C.aj_lm_head_topk_workspace_bytes)
+        self._head_buffers(L, k, "tws", C.aj_lm_head_topk_workspace_bytes)
         self.refresh_transposed()
         idx = torch.empty(L.n_mask, k, dtype=torch.int32, device=self.dev)
         logprob = torch.empty(L.n_mask, k, dtype=torch.float32, device=self.dev)
@@ -360,7 +361,7 @@ class ActorUpdate:
             C.aj_embed_fwd(L.tok[t0:t1], self.W["emb"], x, self.err)
             self._stack_fwd(L.cu_seqlens[s0:s1 + 1], L.pos[t0:t1], p["max_len"], x, y, t0)
             C.aj_lm_head_topk(self.lcfg, L.targets[r0:r1], y, self.W["final_norm"], self.W["w_vocab"],
-                              1.0 / temperature, idx[r0:r1], logprob[r0:r1], lse[r0:r1], self.hws,
+                              1.0 / temperature, idx[r0:r1], logprob[r0:r1], lse[r0:r1], self.tws,
                               row_base=t0, w_vocab_t=self._w_vocab_t(), err=self.err)
         return idx, logprob
 
@@ -375,7 +376,7 @@ class ActorUpdate:
                             f"{L.n_mask} targets")
         if weight is not None and tuple(weight.shape) != (L.n_mask,):
             raise C.AjError(f"distill_step: weight {tuple(weight.shape)} for {L.n_mask} targets")
-        self._head_buffers(L, idx.shape[1], C.aj_lm_head_workspace_bytes)
+        self._head_buffers(L, idx.shape[1], "hws", C.aj_lm_head_workspace_bytes)
         if coef is None:
             coef = 1.0 / L.n_mask if L.n_mask else 0.0
         W, G = self.W, self.G

@@ -183,3 +183,20 @@ def test_lists_that_are_no_matrix():
     flat = torch.zeros(L.n_mask, dtype=torch.int32, device="cuda")
     with pytest.raises(capi.AjError, match="lists"):
         A.distill_step(L, flat, flat.float())
+
+
+def test_teacher_and_student_of_one_object_keep_their_workspaces():
+    """A graph of one call holds on to its workspace while the other is made."""
+    from paper_2606_04484_amd import actor
+    case = Case(workload(get_config(0).model))
+    L = actor.merge(actor.upload_timelines(case.tl, case.old))
+    A = actor.ActorUpdate(case.m, case.device_weights())
+    A.zero_grads()
+    idx, lp = A.teacher_topk(L, 8)
+    at = A.tws.data_ptr()
+    A.distill_step(L, idx, lp)
+    own = A.hws.data_ptr()
+    again = A.teacher_topk(L, 8)
+    torch.cuda.synchronize()
+    assert A.tws.data_ptr() == at and A.hws.data_ptr() == own != at
+    assert torch.equal(again[0], idx) and torch.equal(again[1], lp)
